@@ -490,6 +490,114 @@ int blast_sparse_mlp_events(const blast_bsr_view* Wgate, const blast_bsr_view* W
 int blast_bsr_gated_spmm(const blast_bsr_view* Wgate, const blast_bsr_view* Wup, const uint16_t* X, int64_t ldx,
                          int32_t x_layout, int64_t T, int32_t act, uint16_t* H, int64_t ldh, void* stream);
 
+/*
+ * ---- around the MLP: what a transformer block and its training step put next to the products ----------------------------
+ *
+ * blast_bsr_linear: block-sparse product with bias, activation and residual in its epilogue (a projection of an MLP block as
+ * a model has it, Sec. 2.1; Sec. 3.4.3 fuses the nonlinearity the same way):
+ *     Z = W~ X + bias,   Y = act(Z) + R,
+ * bf16 x bf16 products, fp32 sums, bias, activation and residual added in fp32, one rounding when a value is stored.  A row
+ * of an empty block row is act(bias) + R.
+ *   W, X, ldx, layout, T     as in blast_bsr_spmm (W->aux is not read: rows are never cut into chunks, so sums have a fixed
+ *                            order)
+ *   bias                     fp32 [rows], may be NULL
+ *   act                      BLAST_ACT_NONE, _SILU, _GELU or _RELU
+ *   R, ldr, r_dtype          residual in the layout of X, fp32 or bf16, may be NULL; may be Y itself (same pitch and type)
+ *   Y, ldy, y_dtype          out, in the layout of X, fp32 or bf16
+ *   Z, ldz                   out, bf16 in the layout of X, may be NULL: what blast_act_backward reads; must not overlap Y
+ *   ws, ws_bytes             as in blast_bsr_spmm: blast_bsr_spmm_workspace() bytes, optional
+ * Never synchronises.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED_BLOCK, HIP.
+ */
+#define BLAST_ACT_NONE (-1) /* act(z) = z: blast_bsr_linear and blast_act_backward only */
+int blast_bsr_linear(const blast_bsr_view* W, const uint16_t* X, int64_t ldx, int32_t layout, int64_t T, const float* bias,
+                     int32_t act, const void* R, int64_t ldr, int32_t r_dtype, void* Y, int64_t ldy, int32_t y_dtype,
+                     uint16_t* Z, int64_t ldz, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gradient through the activation and the bias, for the backward products (blast_bsr_transpose, blast_bsr_sddmm):
+ *     single (U NULL):  dZ = dY act'(Z),  dbias_z[n] = sum_t dZ
+ *     gated:            H = act(Z) U,  dZ = dY U act'(Z),  dU = dY act(Z),  dbias_z = sum_t dZ,  dbias_u = sum_t dU
+ * (the first half of Eq. (1) with Z = Wgate X, dY the gradient of H; H is what the gradient of Wdown needs, made again
+ * instead of kept).  All tensors token-major [T][N].  fp32 arithmetic, one rounding when a value is stored; the sums are of
+ * the unrounded values, in fp32 and in a fixed order.  relu'(0) = 0.
+ *   Z, ldz            bf16; may be NULL with BLAST_ACT_NONE and no U (only dY is read then)
+ *   U, ldu            bf16 or NULL
+ *   dY, lddy, dy_dtype   fp32 or bf16
+ *   dZ, dU, H         out, bf16, each with its pitch; any may be NULL; dZ may be Z, dU may be U, and any of the three a bf16 dY
+ *                     (same pitch); each element is read before it is written
+ *   dbias_z, dbias_u  out, fp32 [N], may be NULL; T = 0 gives zeros
+ *   ws, ws_bytes      blast_act_backward_workspace() bytes (0 without bias gradients), 16-byte aligned
+ * Never synchronises.  Errors: INVALID_ARG, WORKSPACE, HIP.
+ */
+int blast_act_backward(const uint16_t* Z, int64_t ldz, const uint16_t* U, int64_t ldu, const void* dY, int64_t lddy,
+                       int32_t dy_dtype, int64_t T, int64_t N, int32_t act, uint16_t* dZ, int64_t lddz, uint16_t* dU,
+                       int64_t lddu, uint16_t* H, int64_t ldh, float* dbias_z, float* dbias_u, void* ws, size_t ws_bytes,
+                       void* stream);
+int blast_act_backward_workspace(int64_t T, int64_t N, int32_t n_bias_grads, size_t* ws_bytes /* HOST */);
+
+#define BLAST_NORM_RMS 0   /* v / sqrt(mean(v^2) + eps) */
+#define BLAST_NORM_LAYER 1 /* (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) */
+
+/* Parameters of the norms around a block.  A plain view like blast_bsr_view: the arrays are device memory, the struct is
+ * read at call time. */
+typedef struct blast_norm_view {
+  int64_t width;             /* features of a row, 1 to BLAST_NORM_MAX_WIDTH */
+  int32_t kind;              /* BLAST_NORM_RMS or BLAST_NORM_LAYER, of both norms */
+  int32_t post;              /* 1: the block's output goes through a norm of its own before it is added */
+  float eps, scale;          /* eps >= 0; scale: factor of the block's output */
+  int32_t p_dtype, g_dtype;  /* BLAST_F32 / BLAST_BF16 of the four parameter arrays / of the gate */
+  const void* weight;        /* [width], NULL = ones */
+  const void* bias;          /* [width], NULL = none; layer norms only, as post_bias */
+  const void* post_weight;   /* of the norm of the block's output; read only with post = 1 */
+  const void* post_bias;
+  const void* gate;          /* NULL: none */
+  int64_t ldg;               /* 0: gate is one row [width] for all tokens, else [T][width] with this pitch */
+} blast_norm_view;
+#define BLAST_NORM_MAX_WIDTH 32768
+
+/*
+ * The step between two blocks of a residual network, in one pass over the data:
+ *     p = post ? norm(y) * post_weight + post_bias : y
+ *     h_out = h + scale * gate * p,    x = norm(h_out) * weight + bias
+ * (y is the output of the block before, x the bf16 operand of the product that follows).  Arithmetic in fp32 with every row
+ * held in registers; the variance is that of the centred values; h_out enters the norm before it is rounded.
+ *   h, ldh, h_dtype     residual stream [T][width], fp32 or bf16
+ *   y, ldy, y_dtype     block output, fp32 or bf16; NULL: x = norm(h) only (gate and post are then not used)
+ *   h_out, ldho         out, h_dtype; may be h (same pitch); required with y, ignored without
+ *   x, ldx, x_dtype     out, fp32 or bf16
+ *   stats               out, fp32 [T][4], may be NULL: mean and reciprocal deviation of h_out, then those of y (0 where
+ *                       there is no such norm; the mean of an RMS norm is 0)
+ * Never synchronises, no workspace.  Errors: INVALID_ARG, HIP.
+ */
+int blast_norm_residual(const blast_norm_view* P, const void* h, int64_t ldh, int32_t h_dtype, const void* y, int64_t ldy,
+                        int32_t y_dtype, int64_t T, void* h_out, int64_t ldho, void* x, int64_t ldx, int32_t x_dtype,
+                        float* stats, void* stream);
+
+/*
+ * Its gradient.  With n = (h_out - mean) r and m = (y - mean_y) r_y from `stats`:
+ *     dh = dh_out + r (dn - n mean(dn n) [- mean(dn)]),  dn = dx * weight          ([..]: layer norm)
+ *     dp = scale * gate * dh,   dgate = scale * dh * p
+ *     dy = post ? r_y (dm - m mean(dm m) [- mean(dm)]),  dm = dp * post_weight : dp
+ *     dweight = sum_t dx n,  dbias = sum_t dx,  dpost_weight = sum_t dp m,  dpost_bias = sum_t dp
+ *   h_out, y, stats     what the forward call wrote and read (y NULL as there)
+ *   dx, lddx, dx_dtype  gradient of x, fp32 or bf16
+ *   dh_out, lddho       gradient of h_out through the rest of the stream, h_dtype, may be NULL (zero)
+ *   dh, lddh            out, h_dtype; may be dh_out (same pitch)
+ *   dy, lddy, dy_dtype  out, fp32 or bf16, may be NULL
+ *   dgate, lddg         out, may be NULL: with P->ldg = 0 fp32 [width], the sum over the tokens; else [T][width] in g_dtype
+ *   dweight, dbias, dpost_weight, dpost_bias   out, fp32 [width], any may be NULL; like a [width] dgate they are summed in
+ *                       fp32 and in a fixed order; T = 0 gives zeros
+ *   ws, ws_bytes        blast_norm_residual_backward_workspace() bytes, 16-byte aligned; scratch of the sums
+ * Never synchronises.  Errors: INVALID_ARG, WORKSPACE, HIP.
+ */
+int blast_norm_residual_backward(const blast_norm_view* P, const void* h_out, int64_t ldho, int32_t h_dtype, const void* y,
+                                 int64_t ldy, int32_t y_dtype, const float* stats, const void* dx, int64_t lddx,
+                                 int32_t dx_dtype, const void* dh_out, int64_t lddho, int64_t T, void* dh, int64_t lddh,
+                                 void* dy, int64_t lddy, int32_t dy_dtype, void* dgate, int64_t lddg, float* dweight,
+                                 float* dbias, float* dpost_weight, float* dpost_bias, void* ws, size_t ws_bytes,
+                                 void* stream);
+int blast_norm_residual_backward_workspace(const blast_norm_view* P, int64_t T, size_t* ws_bytes /* HOST */);
+
 #ifdef __cplusplus
 }
 #endif

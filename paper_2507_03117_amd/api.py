@@ -20,6 +20,8 @@ PACK_MASK, PACK_TOPK_FROBENIUS = 0, 1
 TOKEN_MAJOR, FEATURE_MAJOR, COLUMN_GROUPS_64 = 0, 1, 2
 F32, BF16 = 0, 1
 ACT = {"silu": 0, "gelu": 1, "relu": 2}
+ACT_NONE = -1
+NORM = {"rms": 0, "layer": 1}
 
 EXPORTS = (
     "blast_strerror", "blast_n_keep", "blast_bsr_aux_bytes", "blast_bsr_pack_bound", "blast_bsr_pack", "blast_bsr_pack_enqueue",
@@ -31,6 +33,8 @@ EXPORTS = (
     "blast_bsr_unpack", "blast_bsr_gated_spmm", "blast_bsr_joint_row_order",
     "blast_sparse_mlp_static", "blast_sparse_mlp_static_limit", "blast_sparse_mlp_status",
     "blast_sparse_mlp_handover_test", "blast_sparse_mlp_e5m2w", "blast_sparse_mlp_e5m2w_workspace",
+    "blast_bsr_linear", "blast_act_backward", "blast_act_backward_workspace", "blast_norm_residual",
+    "blast_norm_residual_backward", "blast_norm_residual_backward_workspace",
 )
 
 
@@ -45,6 +49,14 @@ class BsrView(C.Structure):
         ("rows", C.c_int64), ("cols", C.c_int64), ("b", C.c_int32), ("max_row_blocks", C.c_int32), ("nnz", C.c_int64),
         ("row_ptr", C.c_void_p), ("col_idx", C.c_void_p), ("vals", C.c_void_p), ("row_order", C.c_void_p),
         ("aux", C.c_void_p),
+    ]
+
+
+class NormView(C.Structure):
+    _fields_ = [
+        ("width", C.c_int64), ("kind", C.c_int32), ("post", C.c_int32), ("eps", C.c_float), ("scale", C.c_float),
+        ("p_dtype", C.c_int32), ("g_dtype", C.c_int32), ("weight", C.c_void_p), ("bias", C.c_void_p),
+        ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("gate", C.c_void_p), ("ldg", C.c_int64),
     ]
 
 
@@ -128,6 +140,21 @@ def lib():
         L.blast_bsr_joint_row_order.argtypes = [pv, pv, vp, vp]
         L.blast_bsr_gated_spmm.restype = C.c_int
         L.blast_bsr_gated_spmm.argtypes = [pv, pv, vp, i64, i32, i64, i32, vp, i64, vp]
+        L.blast_bsr_linear.restype = C.c_int
+        L.blast_bsr_linear.argtypes = [pv, vp, i64, i32, i64, vp, i32, vp, i64, i32, vp, i64, i32, vp, i64, vp, sz, vp]
+        L.blast_act_backward.restype = C.c_int
+        L.blast_act_backward.argtypes = [vp, i64, vp, i64, vp, i64, i32, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp,
+                                         sz, vp]
+        L.blast_act_backward_workspace.restype = C.c_int
+        L.blast_act_backward_workspace.argtypes = [i64, i64, i32, C.POINTER(sz)]
+        pn = C.POINTER(NormView)
+        L.blast_norm_residual.restype = C.c_int
+        L.blast_norm_residual.argtypes = [pn, vp, i64, i32, vp, i64, i32, i64, vp, i64, vp, i64, i32, vp, vp]
+        L.blast_norm_residual_backward.restype = C.c_int
+        L.blast_norm_residual_backward.argtypes = [pn, vp, i64, i32, vp, i64, i32, vp, vp, i64, i32, vp, i64, i64, vp, i64, vp,
+                                                   i64, i32, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+        L.blast_norm_residual_backward_workspace.restype = C.c_int
+        L.blast_norm_residual_backward_workspace.argtypes = [pn, i64, C.POINTER(sz)]
         _lib = L
     return _lib
 
@@ -576,3 +603,246 @@ def bsr_gated_spmm(gate: PackedBsr, up: PackedBsr, X: torch.Tensor, *, layout: i
     _check(L.blast_bsr_gated_spmm(C.byref(vg), C.byref(vu), _ptr(X), ldx, layout, T, ACT[act], _ptr(H), H.stride(0),
                                   _stream()), "blast_bsr_gated_spmm")
     return H
+
+
+# ---- around the MLP: projections with an epilogue, the gradient of an activation, norms with gate and residual ---------
+
+def _dtype_code(dtype: torch.dtype) -> int:
+    if dtype == torch.float32:
+        return F32
+    assert dtype == torch.bfloat16, "fp32 or bf16"
+    return BF16
+
+
+def _rows_of(t: Optional[torch.Tensor], shape, dtypes):
+    """(address, row pitch) of an operand of that shape with contiguous rows; (None, 0) without one."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and tuple(t.shape) == tuple(shape) and t.dtype in dtypes, (tuple(t.shape), t.dtype, shape)
+    assert t.shape[1] <= 1 or t.stride(1) == 1
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtypes):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dim() == 1 and t.numel() == n and t.dtype in dtypes and (n <= 1 or t.stride(0) == 1)
+    return t.data_ptr()
+
+
+_EITHER = (torch.float32, torch.bfloat16)
+
+
+def _linear_args(W: PackedBsr, X, out, bias, act, residual, pre, layout, ws):
+    T, K, ldx = _layout_dims(X, layout)
+    assert K == W.cols
+    shape = (T, W.rows) if layout == TOKEN_MAJOR else (W.rows, T)
+    y, ldy = _rows_of(out, shape, _EITHER)
+    r, ldr = _rows_of(residual, shape, _EITHER)
+    z, ldz = _rows_of(pre, shape, (torch.bfloat16,))
+    return (X.data_ptr(), ldx, layout, T, _vector(bias, W.rows, (torch.float32,)), ACT_NONE if act is None else ACT[act], r,
+            ldr, F32 if r is None else _dtype_code(residual.dtype), y, ldy, _dtype_code(out.dtype), z, ldz, _ptr(ws),
+            0 if ws is None else ws.numel())
+
+
+def _linear_scratch(W: PackedBsr, T: int, dev) -> Optional[torch.Tensor]:
+    if W.b != 16:  # the only blocks whose product has scratch
+        return None
+    v, wsb = W.view(), C.c_size_t(0)
+    _check(lib().blast_bsr_spmm_workspace(C.byref(v), T, C.byref(wsb)), "blast_bsr_spmm_workspace")
+    return torch.empty(wsb.value, dtype=torch.uint8, device=dev) if wsb.value else None
+
+
+def bsr_linear(W: PackedBsr, X: torch.Tensor, *, bias: Optional[torch.Tensor] = None, act: Optional[str] = None,
+               residual: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, layout: int = TOKEN_MAJOR,
+               out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+               ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """blast_bsr_linear: Y = act(W * X + bias) + residual, with bias fp32 [rows] and residual fp32 or bf16 in Y's layout (it may
+    be `out`).  `pre`: a bf16 tensor that receives W * X + bias, what act_backward reads."""
+    T, _, _ = _layout_dims(X, layout)
+    Y = out if out is not None else _alloc_out(W.rows, T, layout, out_dtype, X.device)
+    if ws is None:
+        ws = _linear_scratch(W, T, X.device)
+    v = W.view()
+    args = _linear_args(W, X, Y, bias, act, residual, pre, layout, ws)
+    _check(lib().blast_bsr_linear(C.byref(v), *args, _stream()), "blast_bsr_linear")
+    return Y
+
+
+def prepare_bsr_linear(W: PackedBsr, X: torch.Tensor, out: torch.Tensor, *, bias: Optional[torch.Tensor] = None,
+                       act: Optional[str] = None, residual: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None,
+                       layout: int = TOKEN_MAJOR, ws: Optional[torch.Tensor] = None) -> PreparedCall:
+    """blast_bsr_linear on the current stream with fixed buffers, as a PreparedCall."""
+    L = lib()
+    if ws is None:
+        ws = _linear_scratch(W, _layout_dims(X, layout)[0], X.device)
+    v = W.view()
+    args = _linear_args(W, X, out, bias, act, residual, pre, layout, ws)
+    types = L.blast_bsr_linear.argtypes
+    args = [C.byref(v)] + [t(a) for t, a in zip(types[1:], args + (_stream(),))]
+    return PreparedCall(L.blast_bsr_linear, "blast_bsr_linear", tuple(args), (v, W, X, out, bias, residual, pre, ws))
+
+
+@dataclass
+class ActGrads:
+    """Gradients of act_backward (dZ, dbias) and gated_act_backward (all but those two)."""
+    dZ: Optional[torch.Tensor] = None  # bf16 [T, N]
+    dbias: Optional[torch.Tensor] = None  # fp32 [N]
+    dG: Optional[torch.Tensor] = None
+    dU: Optional[torch.Tensor] = None
+    H: Optional[torch.Tensor] = None
+    dbias_g: Optional[torch.Tensor] = None
+    dbias_u: Optional[torch.Tensor] = None
+
+
+def _act_backward(Z, U, dY, act, dZ, dU, H, dbias_z, dbias_u):
+    assert dY.dim() == 2
+    L, (T, N) = lib(), dY.shape
+    low, sums = (torch.bfloat16,), (torch.float32,)
+    operands = []
+    for t in (Z, U):
+        operands += _rows_of(t, (T, N), low)
+    operands += _rows_of(dY, (T, N), _EITHER)
+    results = []
+    for t in (dZ, dU, H):
+        results += _rows_of(t, (T, N), low)
+    wanted, ws, wsb = (dbias_z is not None) + (dbias_u is not None), None, C.c_size_t(0)
+    if wanted:
+        _check(L.blast_act_backward_workspace(T, N, wanted, C.byref(wsb)), "blast_act_backward_workspace")
+        ws = torch.empty(wsb.value, dtype=torch.uint8, device=dY.device) if wsb.value else None
+    _check(L.blast_act_backward(*operands, _dtype_code(dY.dtype), T, N, ACT_NONE if act is None else ACT[act], *results,
+                                _vector(dbias_z, N, sums), _vector(dbias_u, N, sums), _ptr(ws), wsb.value, _stream()),
+           "blast_act_backward")
+
+
+def act_backward(Z: Optional[torch.Tensor], dY: torch.Tensor, *, act: Optional[str] = None, bias_grad: bool = False,
+                 out: Optional[torch.Tensor] = None) -> ActGrads:
+    """blast_act_backward of one matrix: dZ = dY * act'(Z) (bf16) and, with bias_grad, dbias = its sum over the tokens.
+    Z: the `pre` of bsr_linear, bf16 [T, N]; None without an activation."""
+    dZ = out if out is not None else torch.empty(dY.shape, dtype=torch.bfloat16, device=dY.device)
+    db = torch.empty(dY.shape[1], dtype=torch.float32, device=dY.device) if bias_grad else None
+    _act_backward(Z, None, dY, act, dZ, None, None, db, None)
+    return ActGrads(dZ=dZ, dbias=db)
+
+
+def gated_act_backward(G: torch.Tensor, U: torch.Tensor, dH: torch.Tensor, *, act: str = "silu", bias_grad: bool = False,
+                       with_h: bool = True) -> ActGrads:
+    """blast_act_backward of the gated product H = act(G) * U: dG, dU and (with_h) H again, bf16; with bias_grad the sums of dG
+    and dU over the tokens."""
+    new = lambda: torch.empty(dH.shape, dtype=torch.bfloat16, device=dH.device)  # noqa: E731
+    col = lambda: torch.empty(dH.shape[1], dtype=torch.float32, device=dH.device) if bias_grad else None  # noqa: E731
+    g = ActGrads(dG=new(), dU=new(), H=new() if with_h else None, dbias_g=col(), dbias_u=col())
+    assert U is not None
+    _act_backward(G, U, dH, act, g.dG, g.dU, g.H, g.dbias_g, g.dbias_u)
+    return g
+
+
+def _norm_view(width, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps) -> NormView:
+    given = [p for p in (weight, bias, post_weight, post_bias) if p is not None]
+    dtype = given[0].dtype if given else torch.float32
+    assert all(p.dtype == dtype for p in given), "weights and biases have one type"
+    p = [_vector(t, width, (dtype,)) if t is not None else None for t in (weight, bias, post_weight, post_bias)]
+    g, ldg, g_dtype = None, 0, torch.float32
+    if gate is not None:
+        g_dtype = gate.dtype
+        if gate.dim() == 1:
+            g = _vector(gate, width, _EITHER)
+        else:
+            g, ldg = _rows_of(gate, (T, width), _EITHER)
+    return NormView(width, NORM[kind], 1 if post else 0, eps, scale, _dtype_code(dtype), _dtype_code(g_dtype), *p, g, ldg)
+
+
+def _norm_args(h, y, h_out, x, stats):
+    assert h.dim() == 2
+    T, E = h.shape
+    hp, ldh = _rows_of(h, (T, E), _EITHER)
+    yp, ldy = _rows_of(y, (T, E), _EITHER)
+    op, ldo = (None, 0) if y is None else _rows_of(h_out, (T, E), (h.dtype,))
+    xp, ldx = _rows_of(x, (T, E), _EITHER)
+    if stats is not None:
+        assert stats.is_cuda and stats.dtype == torch.float32 and tuple(stats.shape) == (T, 4) and stats.is_contiguous()
+    return (hp, ldh, _dtype_code(h.dtype), yp, ldy, F32 if y is None else _dtype_code(y.dtype), T, op, ldo, xp, ldx,
+            _dtype_code(x.dtype), _ptr(stats))
+
+
+def norm_residual(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, kind: str = "rms",
+                  weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, post: bool = False,
+                  post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, scale: float = 1.0, eps: float = 1e-5,
+                  out_dtype: torch.dtype = torch.bfloat16, h_out: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, with_stats: bool = False):
+    """blast_norm_residual: h' = h + scale * gate * (post-)norm(y) and x = norm(h') * weight + bias; returns (h', x), with
+    with_stats (h', x, stats).  Without y: x = norm(h) and h' is h.  gate: [width] or [T, width]; h_out may be h."""
+    new_h = h if y is None else h_out if h_out is not None else torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    x = out if out is not None else torch.empty(h.shape, dtype=out_dtype, device=h.device)
+    stats = torch.empty((h.shape[0], 4), dtype=torch.float32, device=h.device) if with_stats else None
+    v = _norm_view(h.shape[1], h.shape[0], kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
+    _check(lib().blast_norm_residual(C.byref(v), *_norm_args(h, y, new_h, x, stats), _stream()), "blast_norm_residual")
+    return (new_h, x, stats) if with_stats else (new_h, x)
+
+
+def prepare_norm_residual(h: torch.Tensor, y: Optional[torch.Tensor], h_out: torch.Tensor, out: torch.Tensor, *,
+                          stats: Optional[torch.Tensor] = None, kind: str = "rms", weight: Optional[torch.Tensor] = None,
+                          bias: Optional[torch.Tensor] = None, post: bool = False, post_weight: Optional[torch.Tensor] = None,
+                          post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, scale: float = 1.0,
+                          eps: float = 1e-5) -> PreparedCall:
+    """blast_norm_residual on the current stream with fixed buffers, as a PreparedCall."""
+    L = lib()
+    v = _norm_view(h.shape[1], h.shape[0], kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
+    types = L.blast_norm_residual.argtypes
+    args = [C.byref(v)] + [t(a) for t, a in zip(types[1:], _norm_args(h, y, h_out, out, stats) + (_stream(),))]
+    return PreparedCall(L.blast_norm_residual, "blast_norm_residual", tuple(args),
+                        (v, h, y, h_out, out, stats, weight, bias, post_weight, post_bias, gate))
+
+
+@dataclass
+class NormGrads:
+    """Gradients of norm_residual; None where there is no such input."""
+    dh: torch.Tensor  # like h
+    dy: Optional[torch.Tensor]  # [T, width], bf16 unless asked otherwise
+    dgate: Optional[torch.Tensor]  # like the gate; fp32 for a gate of one row
+    dweight: Optional[torch.Tensor]  # fp32 [width], as the following
+    dbias: Optional[torch.Tensor]
+    dpost_weight: Optional[torch.Tensor]
+    dpost_bias: Optional[torch.Tensor]
+
+
+def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats: torch.Tensor, dx: torch.Tensor,
+                           dh_out: Optional[torch.Tensor] = None, *, kind: str = "rms", weight: Optional[torch.Tensor] = None,
+                           bias: Optional[torch.Tensor] = None, post: bool = False,
+                           post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                           gate: Optional[torch.Tensor] = None, scale: float = 1.0, eps: float = 1e-5,
+                           dy_dtype: torch.dtype = torch.bfloat16, dh: Optional[torch.Tensor] = None) -> NormGrads:
+    """blast_norm_residual_backward.  h_out, stats: of the forward call; dx: gradient of x; dh_out: of h_out through the rest of
+    the stream; dh: where the gradient of h goes (it may be dh_out)."""
+    L = lib()
+    assert h_out.dim() == 2
+    T, E = h_out.shape
+    dev = h_out.device
+    v = _norm_view(E, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
+    col = lambda given: torch.empty(E, dtype=torch.float32, device=dev) if given is not None else None  # noqa: E731
+    branch = y is not None
+    g = NormGrads(dh=dh if dh is not None else torch.empty((T, E), dtype=h_out.dtype, device=dev),
+                  dy=torch.empty((T, E), dtype=dy_dtype, device=dev) if branch else None, dgate=None, dweight=col(weight),
+                  dbias=col(bias), dpost_weight=col(post_weight) if branch and post else None,
+                  dpost_bias=col(post_bias) if branch and post else None)
+    if branch and gate is not None:
+        g.dgate = col(gate) if gate.dim() == 1 else torch.empty((T, E), dtype=gate.dtype, device=dev)
+    assert stats.is_cuda and stats.dtype == torch.float32 and tuple(stats.shape) == (T, 4) and stats.is_contiguous()
+    hp, ldh = _rows_of(h_out, (T, E), _EITHER)
+    yp, ldy = _rows_of(y, (T, E), _EITHER)
+    dxp, lddx = _rows_of(dx, (T, E), _EITHER)
+    dhop, lddho = _rows_of(dh_out, (T, E), (h_out.dtype,))
+    dhp, lddh = _rows_of(g.dh, (T, E), (h_out.dtype,))
+    dyp, lddy = _rows_of(g.dy, (T, E), _EITHER)
+    lddg = 0 if g.dgate is None or g.dgate.dim() == 1 else _rows_of(g.dgate, (T, E), _EITHER)[1]
+    wsb, ws = C.c_size_t(0), None
+    _check(L.blast_norm_residual_backward_workspace(C.byref(v), T, C.byref(wsb)), "blast_norm_residual_backward_workspace")
+    if wsb.value:
+        ws = torch.empty(wsb.value, dtype=torch.uint8, device=dev)
+    _check(L.blast_norm_residual_backward(
+        C.byref(v), hp, ldh, _dtype_code(h_out.dtype), yp, ldy, F32 if y is None else _dtype_code(y.dtype), stats.data_ptr(),
+        dxp, lddx, _dtype_code(dx.dtype), dhop, lddho, T, dhp, lddh, dyp, lddy, _dtype_code(dy_dtype), _ptr(g.dgate), lddg,
+        _ptr(g.dweight), _ptr(g.dbias), _ptr(g.dpost_weight), _ptr(g.dpost_bias), _ptr(ws), wsb.value, _stream()),
+        "blast_norm_residual_backward")
+    return g

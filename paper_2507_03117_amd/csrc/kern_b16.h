@@ -283,7 +283,7 @@ __global__ __launch_bounds__(NW * 64, DEPTH ? 4 : 1) void k_spmm_b16(const TileA
 
 // Token-major activations [T][K] (row pitch ld) into column groups of 16 features, [K/16][T][16].  A workgroup
 // turns 16 tokens x 128 features; a half-wave writes the 512 consecutive bytes of one (column group, 16 tokens).
-__global__ __launch_bounds__(256) void k_group16(const uint16_t* __restrict__ X, int64_t ld, int T, int nbc,
+static __global__ __launch_bounds__(256) void k_group16(const uint16_t* __restrict__ X, int64_t ld, int T, int nbc,
                                                  uint16_t* __restrict__ Xg) {
   const int i = threadIdx.x;
   const int half = i & 1, t = (int)blockIdx.x * 16 + ((i >> 1) & 15), c = (int)blockIdx.y * 8 + (i >> 5);

@@ -38,6 +38,23 @@ struct TileArgs {
   int y_grp16;           // ... and so is Y, [rows/16][T][16]
 };
 
+// What a product with an epilogue of its own (blast_bsr_linear) does with a sum, all of it optional: Z = sum + bias, kept in
+// bf16; Y = act(Z) + R.  Rows of R and Z are contiguous (token-major) where a kernel other than the generic one runs.
+struct Epilogue {
+  static constexpr bool kOn = true;
+  const float* bias;   // per row
+  const void* R;       // residual, element strides along tokens / rows
+  int64_t srt, sri;
+  uint16_t* Z;         // bf16
+  int64_t szt, szi;
+  int r_bf16;
+  int act;             // BLAST_ACT_*
+  int pairs;           // two neighbouring rows of a token of R and of Z may be read / stored as one value
+};
+struct NoEpilogue {
+  static constexpr bool kOn = false;
+};
+
 // Index arrays are read-only for the lifetime of a launch: reading them through the
 // constant address space lets uniform loads go through the scalar unit, so they never
 // sit in the vector-memory counter that the DMA pipeline is tracked with.
@@ -71,8 +88,8 @@ __device__ __forceinline__ void store_through(T* p, T v) {
 // to 4096 tokens on the streaming kernel 1 % less time on average.  Rows of one or two blocks under thousands of tokens, whose
 // values hardly ever need the second arm and which multiply little, take up to 4 % more: 1024 and 4096 features at 90 %, 64-wide,
 // 4096 tokens 28.9 / 30.0 us).
-__device__ __forceinline__ float gelu(float g) {
-  const float t = __builtin_fabsf(g);
+// normal_tail: Phi(-t) for t >= 0.
+__device__ __forceinline__ float normal_tail(float t) {
   float r = -5.96657159e-8f;
   r = __builtin_fmaf(r, t, 1.44687544e-6f);
   r = __builtin_fmaf(r, t, -1.56093192e-5f);
@@ -83,7 +100,11 @@ __device__ __forceinline__ float gelu(float g) {
   r = __builtin_fmaf(r, t, -5.24200164e-2f);
   r = __builtin_fmaf(r, t, -4.59224194e-1f);
   r = __builtin_fmaf(r, t, -1.15110409f);
-  const float tail = 0.5f * __builtin_amdgcn_exp2f(t * r);
+  return 0.5f * __builtin_amdgcn_exp2f(t * r);
+}
+
+__device__ __forceinline__ float gelu(float g) {
+  const float t = __builtin_fabsf(g), tail = normal_tail(t);
   // max(g, 0) - |g| tail, rounded once; infinity has no tail (a finite factor), minus infinity has no value (0 g)
   return __builtin_fmaf(-__builtin_fminf(t, 3.402823466e38f), tail, g > 0.0f ? g : 0.0f * g);
 }
@@ -104,6 +125,20 @@ __device__ __forceinline__ float apply_act(int act, float g) {
   if (act == BLAST_ACT_SILU) return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g));
   if (act == BLAST_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678118654752440f));
   return g > 0.0f ? g : 0.0f;
+}
+
+__device__ __forceinline__ float bf16_value(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+
+// One value through the epilogue: the kernels that end with a few values a lane.  `row` counts in the whole matrix.
+__device__ __forceinline__ float epilogue_value(const Epilogue& e, float v, int64_t tok, int64_t row) {
+  if (e.bias) v += e.bias[row];
+  if (e.Z) e.Z[tok * e.szt + row * e.szi] = f32_to_bf16_rne(v);
+  if (e.act >= 0) v = post_act(e.act, v);
+  if (e.R) {
+    const int64_t at = tok * e.srt + row * e.sri;
+    v += e.r_bf16 ? bf16_value(static_cast<const uint16_t*>(e.R)[at]) : static_cast<const float*>(e.R)[at];
+  }
+  return v;
 }
 
 }  // namespace blast_dev

@@ -126,8 +126,8 @@ __device__ __forceinline__ void run_row(const TileArgs& a, const MatDev& m, int 
 
 // One workgroup = one (block row, token tile).  DUAL: two matrices with the same
 // shape share the tile; the epilogue writes bf16 act(acc0) * acc1.
-template <int B, bool DUAL, bool POST = false>
-__global__ __launch_bounds__(256) void k_spmm_tile(const TileArgs a) {
+template <int B, bool DUAL, bool POST, class EPI>
+__device__ __forceinline__ void spmm_tile(const TileArgs& a, const EPI& epi) {
   static_assert(!(POST && DUAL), "an activation on the output belongs to the single-matrix product");
   using C = TileCfg<B>;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -186,7 +186,8 @@ __global__ __launch_bounds__(256) void k_spmm_tile(const TileArgs a) {
       for (int j = 0; j < 16; ++j) {
         const int tok = t0 + tw * 64 + mi * 32 + 8 * (j / 4) + 4 * lh + (j % 4);
         if (tok < a.T) {
-          const float v = acc0[mi][ni][j];
+          float v = acc0[mi][ni][j];
+          if constexpr (EPI::kOn) v = epilogue_value(epi, v, tok, row);
           const int64_t off = (int64_t)tok * a.syt + row * a.syi;
           if (a.y_bf16)
             reinterpret_cast<uint16_t*>(a.Y)[off] = f32_to_bf16_rne(v);
@@ -197,5 +198,14 @@ __global__ __launch_bounds__(256) void k_spmm_tile(const TileArgs a) {
     }
 }
 
+template <int B, bool DUAL, bool POST = false>
+__global__ __launch_bounds__(256) void k_spmm_tile(const TileArgs a) {
+  spmm_tile<B, DUAL, POST>(a, NoEpilogue{});
+}
+
+template <int B>
+__global__ __launch_bounds__(256) void k_linear_tile(const TileArgs a, const Epilogue epi) {
+  spmm_tile<B, false, false>(a, epi);
+}
 
 }  // namespace blast_dev
