@@ -96,7 +96,7 @@ int launch_fp8_stream(const Fp8Args& f, hipStream_t stream) {
                                         (int)C::LDS_BYTES));
       lds_set.set(dev);
     }
-    kernel<<<dim3((unsigned)grid), dim3(64 * NW), C::LDS_BYTES, stream>>>(sa);
+    kernel<<<dim3((unsigned)grid), dim3(64 * NW), C::LDS_BYTES, stream>>>(sa, NoEpilogue{});
     BLAST_LAUNCH_CHECK("k_spmm_stream (E5M2)");
     return BLAST_OK;
   };

@@ -4,18 +4,10 @@
 
 namespace {
 
-template <int B>
-int launch_linear_tile(TileArgs a, const Epilogue& e, hipStream_t stream) {
-  using C = TileCfg<B>;
-  a.ntt = (a.T + C::TT - 1) / C::TT;
-  const int64_t grid = (int64_t)a.ntt * a.nbr;
-  if (grid <= 0) return BLAST_OK;
-  if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
-  static blast::DeviceFlags lds_set;
-  if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_linear_tile<B>), C::LDS_BYTES, lds_set)) return rc;
-  k_linear_tile<B><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, e);
-  BLAST_LAUNCH_CHECK("k_linear_tile");
-  return BLAST_OK;
+// 32-bit offsets inside a tile's 256 rows, as y_fast.
+bool rows_near(const void* p, int64_t ld) { return !p || (int64_t)257 * ld * 4 < ((int64_t)1 << 31); }
+bool rows_paired(const void* p, int64_t ld, int64_t value_bytes) {
+  return !p || (ld % 2 == 0 && blast::aligned(p, 2 * (size_t)value_bytes));
 }
 
 }  // namespace
@@ -57,12 +49,23 @@ extern "C" int blast_bsr_linear(const blast_bsr_view* W, const uint16_t* X, int6
   } else {
     e.srt = 1, e.sri = ldr, e.szt = 1, e.szi = ldz;
   }
-  (void)ws;
-  (void)ws_bytes;
-  switch (W->b) {
-    case 16: return launch_linear_tile<16>(a, e, stream);
-    case 32: return launch_linear_tile<32>(a, e, stream);
-    case 64: return launch_linear_tile<64>(a, e, stream);
-    default: return launch_linear_tile<128>(a, e, stream);
+  e.pairs = rows_paired(R, ldr, e.r_bf16 ? 2 : 4) && rows_paired(Z, ldz, 2);
+  // feature-major operands, and pitches beyond 32-bit offsets, take the generic kernel
+  if (layout != BLAST_TOKEN_MAJOR || !a.y_fast || !rows_near(R, ldr) || !rows_near(Z, ldz)) {
+    switch (W->b) {
+      case 16: return launch_tile<16, false>(a, stream, e);
+      case 32: return launch_tile<32, false>(a, stream, e);
+      case 64: return launch_tile<64, false>(a, stream, e);
+      default: return launch_tile<128, false>(a, stream, e);
+    }
   }
+  if (group16_applies(W->b, layout, X, ldx, T) && ws && blast::aligned(ws, 16) && ws_bytes >= group16_bytes(W->cols, T)) {
+    uint16_t* Xg = static_cast<uint16_t*>(ws);
+    if (int rc = enqueue_group16(X, ldx, T, W->cols, Xg, stream)) return rc;
+    a.X = Xg;
+    a.x_grp16 = 1;
+  }
+  ChunkPlan plan{};  // (rows are never cut into chunks: the epilogue needs complete sums)
+  plan.fullest = W->max_row_blocks;
+  return dispatch_tile<false>(W->b, a, W->nnz, stream, plan, false, e);
 }

@@ -604,7 +604,7 @@ int launch_decode_w8_ntt(const TileArgs& a, const ChunkPlan& plan, hipStream_t s
     k_zero_shared_rows<B><<<dim3((unsigned)plan.max_chunks, (unsigned)((a.T + 63) / 64)), dim3(256), 0, stream>>>(sa);
     BLAST_LAUNCH_CHECK("k_zero_shared_rows");
   }
-  k_decode<B, DUAL, NTT, CHUNK, XSMALL, false, true><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(d);
+  k_decode<B, DUAL, NTT, CHUNK, XSMALL, false, true><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(d, NoEpilogue{});
   BLAST_LAUNCH_CHECK("k_decode (E5M2 weights)");
   return BLAST_OK;
 }

@@ -191,8 +191,9 @@ __device__ __forceinline__ void b16_join(f32x4_b16 (&acc)[NS]) {
 // the row's pairs among themselves and the partial sums meet in LDS - there are too few rows to fill the chip
 // with a wave each, and a row walked by one wave is a chain of dependent loads.
 // DEPTH > 0: X in column groups, b16_walk with that many pairs in flight; 0: either layout of X, b16_row.
-template <bool DUAL, bool POST, int NS, bool SPLIT = false, int NW = 4, int DEPTH = 0>
-__global__ __launch_bounds__(NW * 64, DEPTH ? 4 : 1) void k_spmm_b16(const TileArgs a, const int y_vec) {
+// EPI: Epilogue: the sums of a single-matrix product go through it.
+template <bool DUAL, bool POST, int NS, bool SPLIT = false, int NW = 4, int DEPTH = 0, class EPI = NoEpilogue>
+__global__ __launch_bounds__(NW * 64, DEPTH ? 4 : 1) void k_spmm_b16(const TileArgs a, const int y_vec, const EPI epi) {
   static_assert(SPLIT || NW == 4, "without SPLIT a workgroup is four independent waves");
   static_assert(!(POST && DUAL), "an activation on the output belongs to the single-matrix product");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -258,6 +259,10 @@ __global__ __launch_bounds__(NW * 64, DEPTH ? 4 : 1) void k_spmm_b16(const TileA
   for (int s = 0; s < NS; ++s) {
     const int t = t0 + s * 16 + (lane & 15);
     if (t >= a.T) continue;
+    if constexpr (EPI::kOn) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc0[s][j] = epilogue_value(epi, acc0[s][j], t, row0 + j);
+    }
     if (y_vec) {
       const int64_t off = a.y_grp16 ? ((int64_t)r * a.T + t) * 16 + (lane >> 4) * 4 : (int64_t)t * a.syt + row0;
       if (a.y_bf16) {

@@ -50,9 +50,17 @@ struct Epilogue {
   int r_bf16;
   int act;             // BLAST_ACT_*
   int pairs;           // two neighbouring rows of a token of R and of Z may be read / stored as one value
+  // the same for the tokens from t0 on
+  Epilogue from(int64_t t0) const {
+    Epilogue e = *this;
+    if (R) e.R = static_cast<const char*>(R) + t0 * srt * (r_bf16 ? 2 : 4);
+    if (Z) e.Z = Z + t0 * szt;
+    return e;
+  }
 };
 struct NoEpilogue {
   static constexpr bool kOn = false;
+  NoEpilogue from(int64_t) const { return *this; }
 };
 
 // Index arrays are read-only for the lifetime of a launch: reading them through the

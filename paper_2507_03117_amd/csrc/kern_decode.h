@@ -288,8 +288,12 @@ struct DecCfg {
 // POST: a single-matrix product whose sums go through the activation a.act before they are stored (the
 // first half of a two-matrix MLP).
 // TAGGED: a producer whose consumers read tagged words (see decode_consumer_tagged).
-template <int B, bool DUAL, int NTT, bool CHUNK, int XSMALL, int ROLE, bool POST = false, bool W8 = false, bool TAGGED = false>
-__device__ __forceinline__ void decode_unit(const DecArgs& a, const int unit, const int t_base, unsigned char* smem) {
+// EPI: Epilogue: the sums of a single-matrix product go through it.
+template <int B, bool DUAL, int NTT, bool CHUNK, int XSMALL, int ROLE, bool POST = false, bool W8 = false, bool TAGGED = false,
+          class EPI = NoEpilogue>
+__device__ __forceinline__ void decode_unit(const DecArgs& a, const int unit, const int t_base, unsigned char* smem,
+                                            const EPI& epi = EPI{}) {
+  static_assert(!EPI::kOn || (!DUAL && !CHUNK && ROLE == kDecAlone && !POST && !W8), "an epilogue of its own has the plain product");
   static_assert(!W8 || ROLE == kDecAlone, "one-byte weights run as ordinary launches");
   static_assert(!(DUAL && CHUNK), "the activation needs complete sums: the gated product is never split");
   static_assert(!POST || (!DUAL && !CHUNK), "an activation on the output needs complete sums of a single matrix");
@@ -658,6 +662,7 @@ __device__ __forceinline__ void decode_unit(const DecArgs& a, const int unit, co
         float v = acc[0][tt][j];
         if (DUAL) v = apply_act(a.act, v) * acc[NM - 1][tt][j];
         if (POST) v = apply_act(a.act, v);
+        if constexpr (EPI::kOn) v = epilogue_value(epi, v, tok, row);
         const int64_t off = (int64_t)tok * a.syt + row * a.syi;
         if (TAGGED) {  // value and tag in one word: whoever sees the tag has the value
           if (!a.withhold)
@@ -815,8 +820,8 @@ __device__ __forceinline__ void decode_consumer_tagged(const DecArgs& a, const i
   }
 }
 
-template <int B, bool DUAL, int NTT, bool CHUNK, int XSMALL, bool POST = false, bool W8 = false>
-__global__ __launch_bounds__(256) void k_decode(const DecArgs a) {
+template <int B, bool DUAL, int NTT, bool CHUNK, int XSMALL, bool POST = false, bool W8 = false, class EPI = NoEpilogue>
+__global__ __launch_bounds__(256) void k_decode(const DecArgs a, const EPI epi) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   // More tokens than one tile holds mean more workgroups per unit, each re-reading the unit's weight
   // slices.  Workgroup ids are dealt round-robin to the 8 XCDs, so the token groups of one unit are
@@ -829,7 +834,7 @@ __global__ __launch_bounds__(256) void k_decode(const DecArgs a) {
   const int rem = blk % span;
   const int unit = (blk / span) * 8 + (rem & 7);
   if (unit >= a.n_units) return;
-  decode_unit<B, DUAL, NTT, CHUNK, XSMALL, kDecAlone, POST, W8>(a, unit, (rem >> 3) * (NTT * 16), smem);
+  decode_unit<B, DUAL, NTT, CHUNK, XSMALL, kDecAlone, POST, W8, false>(a, unit, (rem >> 3) * (NTT * 16), smem, epi);
 }
 
 // Single-launch MLP for one token tile (T <= 16 NTT): workgroups [0, n_units) compute H slice by slice

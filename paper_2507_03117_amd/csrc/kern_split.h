@@ -44,9 +44,10 @@ struct SplitCfg {
   static_assert(sizeof(float) * 64 * 64 == STAGE, "a wave's sums go over its stage");
 };
 
-template <int B, bool POST, int NWAVES>
+// EPI: Epilogue: the sums go through it.
+template <int B, bool POST, int NWAVES, class EPI = NoEpilogue>
 __global__ __launch_bounds__(64 * NWAVES, 2) void k_spmm_split(const TileArgs a, const int n_units, const int groups,
-                                                               const int stride_log2) {
+                                                               const int stride_log2, const EPI epi) {
   using C = SplitCfg<B, NWAVES>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -163,6 +164,7 @@ __global__ __launch_bounds__(64 * NWAVES, 2) void k_spmm_split(const TileArgs a,
       auto pair = [&](int w) { return C::SETS == 2 ? part[w] : part[w] + part[(w + 4) % C::NW]; };
       const float sum = ((pair(0) + pair(1)) + pair(2)) + pair(3);
       y[nj] = POST ? post_act(a.act, sum) : sum;
+      if constexpr (EPI::kOn) y[nj] = epilogue_value(epi, sum, t, row + nj);
     }
     const int64_t off = (int64_t)t * a.syt + row * a.syi;
     typedef __bf16 Bf16Pair __attribute__((ext_vector_type(2)));

@@ -441,6 +441,127 @@ __device__ __forceinline__ void stream_zero_side(const StreamArgs& sa, int w, in
   }
 }
 
+// Bias, Z, activation and residual on a wave's 64-token tile of sums, in registers.  Residual values are asked for
+// 32 tokens at a time before the first is used; addresses are a uniform base, a token step in a scalar register and one
+// 32-bit offset a lane, as where Y is stored.
+template <class C, int B>
+__device__ __forceinline__ void stream_epilogue(const Epilogue& e, f32x16 (&acc)[C::MI][C::NI], int r, int t0, int tw, int rw, int l32,
+                                                int lh, int left) {
+  const int row0 = r * B + rw * C::WT_ROW + C::row_of(l32, 0), lane_left = left - 4 * lh, tok0 = tw * 64 + 4 * lh;
+  constexpr int kStep = C::PAIR ? 1 : 32;  // rows between a lane's values of a token
+  if (e.bias) {
+#pragma unroll
+    for (int ni = 0; ni < C::NI; ++ni) {
+      const float b = e.bias[row0 + ni * kStep];
+#pragma unroll
+      for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[mi][ni][j] += b;
+    }
+  }
+  const bool full = left >= 64;
+  auto store_z = [&](auto whole) {
+    unsigned char* base = reinterpret_cast<unsigned char*>(e.Z + (int64_t)t0 * e.szt);
+    uint32_t pitch = (uint32_t)e.szt * 2u;
+    asm volatile("" : "+s"(pitch));  // (see the stores of Y)
+    const uint32_t off0 = (uint32_t)row0 * 2u + (uint32_t)tok0 * pitch;
+#pragma unroll
+    for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int dt = mi * 32 + 8 * (j / 4) + (j % 4);
+        unsigned char* p = base + __builtin_amdgcn_readfirstlane((uint32_t)dt * pitch) + off0;
+        if (whole.value || dt < lane_left) {
+          if constexpr (C::PAIR) {
+            typedef __bf16 Bf16Pair __attribute__((ext_vector_type(2)));
+            *reinterpret_cast<Bf16Pair*>(p) = Bf16Pair{static_cast<__bf16>(acc[mi][0][j]), static_cast<__bf16>(acc[mi][1][j])};
+          } else {
+#pragma unroll
+            for (int ni = 0; ni < C::NI; ++ni) *reinterpret_cast<uint16_t*>(p + ni * kStep * 2) = f32_to_bf16_rne(acc[mi][ni][j]);
+          }
+        }
+      }
+  };
+  if (e.Z) {
+    if (full)
+      store_z(std::true_type{});
+    else
+      store_z(std::false_type{});
+  }
+  if (e.act >= 0) {
+    auto apply = [&](auto act) {
+#pragma unroll
+      for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < C::NI; ++ni)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) acc[mi][ni][j] = post_act(act.value, acc[mi][ni][j]);
+    };
+    // the branch on the activation stays outside the unrolled loops: one copy of each function body
+    if (e.act == BLAST_ACT_GELU)
+      apply(std::integral_constant<int, BLAST_ACT_GELU>{});
+    else if (e.act == BLAST_ACT_SILU)
+      apply(std::integral_constant<int, BLAST_ACT_SILU>{});
+    else
+      apply(std::integral_constant<int, BLAST_ACT_RELU>{});
+  }
+  if (e.R) {
+    auto add = [&](auto bf16, auto whole) {
+      constexpr uint32_t kEsz = bf16.value ? 2u : 4u;
+      const unsigned char* base = static_cast<const unsigned char*>(e.R) + (int64_t)t0 * e.srt * kEsz;
+      uint32_t pitch = (uint32_t)e.srt * kEsz;
+      asm volatile("" : "+s"(pitch));
+      const uint32_t off0 = (uint32_t)row0 * kEsz + (uint32_t)tok0 * pitch;
+#pragma unroll
+      for (int mi = 0; mi < C::MI; ++mi) {
+        uint32_t v[16][C::NI];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (!whole.value) {
+#pragma unroll
+            for (int ni = 0; ni < C::NI; ++ni) v[j][ni] = 0;
+          }
+          const int dt = mi * 32 + 8 * (j / 4) + (j % 4);
+          const unsigned char* p = base + __builtin_amdgcn_readfirstlane((uint32_t)dt * pitch) + off0;
+          if (whole.value || dt < lane_left) {
+            if constexpr (C::PAIR && bf16.value) {
+              v[j][0] = *reinterpret_cast<const uint32_t*>(p);
+            } else if constexpr (C::PAIR) {
+              const uint2 q = *reinterpret_cast<const uint2*>(p);
+              v[j][0] = q.x;
+              v[j][1] = q.y;
+            } else {
+#pragma unroll
+              for (int ni = 0; ni < C::NI; ++ni)
+                v[j][ni] = bf16.value ? *reinterpret_cast<const uint16_t*>(p + ni * kStep * kEsz)
+                                      : *reinterpret_cast<const uint32_t*>(p + ni * kStep * kEsz);
+            }
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+#pragma unroll
+          for (int ni = 0; ni < C::NI; ++ni) {
+            uint32_t q = v[j][C::PAIR && bf16.value ? 0 : ni];
+            if (bf16.value) q = C::PAIR && ni == 1 ? q & 0xFFFF0000u : q << 16;
+            acc[mi][ni][j] += __uint_as_float(q);
+          }
+      }
+    };
+    if (e.r_bf16) {
+      if (full)
+        add(std::true_type{}, std::true_type{});
+      else
+        add(std::true_type{}, std::false_type{});
+    } else {
+      if (full)
+        add(std::false_type{}, std::true_type{});
+      else
+        add(std::false_type{}, std::false_type{});
+    }
+  }
+}
+
 // CHUNK: the items are (chunk of a block row, token tile) pairs from the packer's chunk plan instead of
 // (block row, token tile); a row made of several chunks adds its partial sums into a zeroed fp32 output.
 // POST: a single-matrix product whose result goes through the activation a.act before it is stored
@@ -448,8 +569,11 @@ __device__ __forceinline__ void stream_zero_side(const StreamArgs& sa, int w, in
 // LONG: the gated product with its long rows cut into chunks and finished by a later launch, see StreamArgs.
 // F8: both operands in E5M2 (MatDev::vals8; X bytes).
 // PAIRS: the lanes hold row pairs (StreamCfg::PAIR), for outputs that take them (y_pairs); false: the instance for others.
-template <int B, bool DUAL, int TW, bool CHUNK, bool POST = false, int NW = 4, bool LONG = false, bool F8 = false, bool PAIRS = true>
-__global__ __launch_bounds__(64 * NW, (StreamCfg<B, TW, NW, F8>::WAVES_PER_SIMD)) void k_spmm_stream(const StreamArgs sa) {
+// EPI: Epilogue, whose operands' rows are contiguous (and, with PAIRS, paired): a single-matrix product without CHUNK or POST.
+template <int B, bool DUAL, int TW, bool CHUNK, bool POST = false, int NW = 4, bool LONG = false, bool F8 = false, bool PAIRS = true,
+          class EPI = NoEpilogue>
+__global__ __launch_bounds__(64 * NW, (StreamCfg<B, TW, NW, F8>::WAVES_PER_SIMD)) void k_spmm_stream(const StreamArgs sa, const EPI epi) {
+  static_assert(!EPI::kOn || (!DUAL && !CHUNK && !POST && !LONG && !F8), "an epilogue of its own has the plain product");
   static_assert(!F8 || (!DUAL && !CHUNK && !POST && !LONG), "the E5M2 product is a plain one");
   static_assert(!(DUAL && CHUNK), "the activation needs complete sums: the gated product is never split");
   static_assert(!POST || (!DUAL && !CHUNK), "an activation on the output needs complete sums of a single matrix");
@@ -852,6 +976,7 @@ __global__ __launch_bounds__(64 * NW, (StreamCfg<B, TW, NW, F8>::WAVES_PER_SIMD)
     const int left = a.T - (t0 + tw * 64);
     if (left <= 0) continue;
     const bool full = left >= 64;
+    if constexpr (EPI::kOn) stream_epilogue<C, B>(epi, acc0, r, t0, tw, rw, l32, lh, left);
     // Fast path (rows contiguous in memory, no atomics, offsets inside the tile fit 32 bits): one uniform 64-bit base
     // per item and a 32-bit lane offset per store, so that a stored value costs a conversion, an add and the store
     // instead of 64-bit address arithmetic; in a tile that the tokens end in, a comparison as well.  (A tile of 40 of

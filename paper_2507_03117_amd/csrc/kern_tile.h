@@ -126,8 +126,9 @@ __device__ __forceinline__ void run_row(const TileArgs& a, const MatDev& m, int 
 
 // One workgroup = one (block row, token tile).  DUAL: two matrices with the same
 // shape share the tile; the epilogue writes bf16 act(acc0) * acc1.
-template <int B, bool DUAL, bool POST, class EPI>
-__device__ __forceinline__ void spmm_tile(const TileArgs& a, const EPI& epi) {
+// EPI: Epilogue: the sums of a single-matrix product go through it.
+template <int B, bool DUAL, bool POST = false, class EPI = NoEpilogue>
+__global__ __launch_bounds__(256) void k_spmm_tile(const TileArgs a, const EPI epi) {
   static_assert(!(POST && DUAL), "an activation on the output belongs to the single-matrix product");
   using C = TileCfg<B>;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -198,14 +199,5 @@ __device__ __forceinline__ void spmm_tile(const TileArgs& a, const EPI& epi) {
     }
 }
 
-template <int B, bool DUAL, bool POST = false>
-__global__ __launch_bounds__(256) void k_spmm_tile(const TileArgs a) {
-  spmm_tile<B, DUAL, POST>(a, NoEpilogue{});
-}
-
-template <int B>
-__global__ __launch_bounds__(256) void k_linear_tile(const TileArgs a, const Epilogue epi) {
-  spmm_tile<B, false, false>(a, epi);
-}
 
 }  // namespace blast_dev

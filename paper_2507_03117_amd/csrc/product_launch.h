@@ -29,26 +29,31 @@ int ensure_lds_limit(const void* kernel, size_t bytes, blast::DeviceFlags& done)
   return BLAST_OK;
 }
 
-template <int B, bool DUAL>
-int launch_tile(TileArgs a, hipStream_t stream) {
+template <int B, bool DUAL, class EPI = NoEpilogue>
+int launch_tile(TileArgs a, hipStream_t stream, const EPI& epi = EPI{}) {
   using C = TileCfg<B>;
   a.ntt = (a.T + C::TT - 1) / C::TT;
   const int64_t grid = (int64_t)a.ntt * a.nbr;
   if (grid <= 0) return BLAST_OK;
   if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
-  if constexpr (!DUAL) {
-    if (a.act >= 0) {  // single matrix with an activation on the output
-      static blast::DeviceFlags lds_set_post;
-      if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, false, true>), C::LDS_BYTES, lds_set_post))
-        return rc;
-      k_spmm_tile<B, false, true><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a);
-      BLAST_LAUNCH_CHECK("k_spmm_tile");
-      return BLAST_OK;
-    }
-  }
   static blast::DeviceFlags lds_set;
-  if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, DUAL>), C::LDS_BYTES, lds_set)) return rc;
-  k_spmm_tile<B, DUAL><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a);
+  if constexpr (EPI::kOn) {
+    if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, false, false, EPI>), C::LDS_BYTES, lds_set)) return rc;
+    k_spmm_tile<B, false, false, EPI><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, epi);
+  } else {
+    if constexpr (!DUAL) {
+      if (a.act >= 0) {  // single matrix with an activation on the output
+        static blast::DeviceFlags lds_set_post;
+        if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, false, true>), C::LDS_BYTES, lds_set_post))
+          return rc;
+        k_spmm_tile<B, false, true><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, NoEpilogue{});
+        BLAST_LAUNCH_CHECK("k_spmm_tile");
+        return BLAST_OK;
+      }
+    }
+    if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, DUAL>), C::LDS_BYTES, lds_set)) return rc;
+    k_spmm_tile<B, DUAL><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, NoEpilogue{});
+  }
   BLAST_LAUNCH_CHECK("k_spmm_tile");
   return BLAST_OK;
 }
@@ -57,14 +62,14 @@ int launch_tile(TileArgs a, hipStream_t stream) {
 // operands straight from global memory.  A wave takes 16, 32 or 64 tokens of one block row.
 int cu_count();
 
-template <bool DUAL, bool POST, int NS, bool SPLIT, int NW = 4, int DEPTH = 0>
-int launch_b16_ns(TileArgs a, int y_vec, hipStream_t stream) {
+template <bool DUAL, bool POST, int NS, bool SPLIT, int NW = 4, int DEPTH = 0, class EPI = NoEpilogue>
+int launch_b16_ns(TileArgs a, int y_vec, hipStream_t stream, const EPI& epi) {
   a.ntt = (a.T + 16 * NS - 1) / (16 * NS);
   const int64_t items = (int64_t)a.ntt * a.nbr;
   const int64_t grid = SPLIT ? items : (items + 3) / 4;
   if (grid <= 0) return BLAST_OK;
   if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
-  k_spmm_b16<DUAL, POST, NS, SPLIT, NW, DEPTH><<<dim3((unsigned)grid), dim3(NW * 64), 0, stream>>>(a, y_vec);
+  k_spmm_b16<DUAL, POST, NS, SPLIT, NW, DEPTH, EPI><<<dim3((unsigned)grid), dim3(NW * 64), 0, stream>>>(a, y_vec, epi);
   BLAST_LAUNCH_CHECK("k_spmm_b16");
   return BLAST_OK;
 }
@@ -73,13 +78,13 @@ int launch_b16_ns(TileArgs a, int y_vec, hipStream_t stream) {
 // shares one (block row, token tile) and its waves deal the row's blocks: 1B-shaped layer, 128 tokens,
 // 31 -> 19 us per MLP pass, 512 tokens 39 -> 32.  Up to 16 tokens, rows of more than 16 pairs on average go to
 // sixteen waves instead of four (the 1B-shaped down projection: 128 rows of 51 blocks).
-template <bool DUAL, bool POST>
-int launch_b16_t(const TileArgs& a, int64_t nnz, int y_vec, hipStream_t stream) {
+template <bool DUAL, bool POST, class EPI>
+int launch_b16_t(const TileArgs& a, int64_t nnz, int y_vec, hipStream_t stream, const EPI& epi) {
   if (a.T <= 16) {
-    if (nnz > (int64_t)32 * a.nbr) return launch_b16_ns<DUAL, POST, 1, true, 16>(a, y_vec, stream);
-    return launch_b16_ns<DUAL, POST, 1, true>(a, y_vec, stream);
+    if (nnz > (int64_t)32 * a.nbr) return launch_b16_ns<DUAL, POST, 1, true, 16>(a, y_vec, stream, epi);
+    return launch_b16_ns<DUAL, POST, 1, true>(a, y_vec, stream, epi);
   }
-  if (a.T <= 32) return launch_b16_ns<DUAL, POST, 2, true>(a, y_vec, stream);
+  if (a.T <= 32) return launch_b16_ns<DUAL, POST, 2, true>(a, y_vec, stream, epi);
   const bool split = (int64_t)((a.T + 63) / 64) * a.nbr < 8 * cu_count();
   // (column groups that 32-bit byte offsets reach, a wave's 64 tokens past the end included)
   if (a.x_grp16 && ((int64_t)a.kdim / 16 * a.T + 64) * 32 < ((int64_t)1 << 32)) {
@@ -93,20 +98,20 @@ int launch_b16_t(const TileArgs& a, int64_t nnz, int y_vec, hipStream_t stream) 
     const int tiles = (a.T + 63) / 64;
     const bool two = (tiles <= 32 && 32 % tiles == 0) || (split ? (int64_t)tiles * a.nbr <= cu_count() : tiles <= 8);
     if (split)
-      return two ? launch_b16_ns<DUAL, POST, 4, true, 4, 2>(a, y_vec, stream) : launch_b16_ns<DUAL, POST, 4, true, 4, 1>(a, y_vec, stream);
-    return two ? launch_b16_ns<DUAL, POST, 4, false, 4, 2>(a, y_vec, stream) : launch_b16_ns<DUAL, POST, 4, false, 4, 1>(a, y_vec, stream);
+      return two ? launch_b16_ns<DUAL, POST, 4, true, 4, 2>(a, y_vec, stream, epi) : launch_b16_ns<DUAL, POST, 4, true, 4, 1>(a, y_vec, stream, epi);
+    return two ? launch_b16_ns<DUAL, POST, 4, false, 4, 2>(a, y_vec, stream, epi) : launch_b16_ns<DUAL, POST, 4, false, 4, 1>(a, y_vec, stream, epi);
   }
-  if (split) return launch_b16_ns<DUAL, POST, 4, true>(a, y_vec, stream);
-  return launch_b16_ns<DUAL, POST, 4, false>(a, y_vec, stream);
+  if (split) return launch_b16_ns<DUAL, POST, 4, true>(a, y_vec, stream, epi);
+  return launch_b16_ns<DUAL, POST, 4, false>(a, y_vec, stream, epi);
 }
 
-template <bool DUAL>
-int launch_b16(const TileArgs& a, int64_t nnz, hipStream_t stream) {
+template <bool DUAL, class EPI>
+int launch_b16(const TileArgs& a, int64_t nnz, hipStream_t stream, const EPI& epi) {
   const int y_vec = a.y_grp16 || (a.syi == 1 && a.syt % 4 == 0 && blast::aligned(a.Y, a.y_bf16 ? 8 : 16));
-  if constexpr (!DUAL) {
-    if (a.act >= 0) return launch_b16_t<false, true>(a, nnz, y_vec, stream);  // an activation on the output
+  if constexpr (!DUAL && !EPI::kOn) {
+    if (a.act >= 0) return launch_b16_t<false, true>(a, nnz, y_vec, stream, epi);  // an activation on the output
   }
-  return launch_b16_t<DUAL, false>(a, nnz, y_vec, stream);
+  return launch_b16_t<DUAL, false>(a, nnz, y_vec, stream, epi);
 }
 
 // From this many tokens on, a product with 16-wide blocks reads its activations from column groups of 16
@@ -187,8 +192,8 @@ struct ChunkPlan {
   int64_t max_chunks1 = 0;
 };
 
-template <int B, bool DUAL, int TW, bool CHUNK, int NW = 4, bool LONG = false>
-int launch_stream_tw(TileArgs a, const ChunkPlan& plan, int64_t k_features, hipStream_t stream) {
+template <int B, bool DUAL, int TW, bool CHUNK, int NW = 4, bool LONG = false, class EPI = NoEpilogue>
+int launch_stream_tw(TileArgs a, const ChunkPlan& plan, int64_t k_features, hipStream_t stream, const EPI& epi = EPI{}) {
   using C = StreamCfg<B, TW, NW>;
   a.ntt = (a.T + C::TT - 1) / C::TT;
   const int64_t n_rows = CHUNK ? plan.max_chunks : (int64_t)a.nbr + (LONG ? plan.max_chunks + plan.max_chunks1 : 0);
@@ -203,6 +208,20 @@ int launch_stream_tw(TileArgs a, const ChunkPlan& plan, int64_t k_features, hipS
   sa.chunk_ke = plan.chunk_ke;
   const int64_t slab = ((int64_t)a.ntt + 7) / 8 * C::TT * k_features * 2;
   const int64_t grid = stream_grid<C, B>(sa, n_rows, cu_count(), slab);
+  if constexpr (EPI::kOn) {
+    auto launch = [&](auto pairs) -> int {
+      constexpr auto kernel = &k_spmm_stream<B, false, TW, false, false, NW, false, false, pairs.value, EPI>;
+      static blast::DeviceFlags lds_set;
+      if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(kernel), C::LDS_BYTES, lds_set)) return rc;
+      kernel<<<dim3((unsigned)grid), dim3(64 * NW), C::LDS_BYTES, stream>>>(sa, epi);
+      BLAST_LAUNCH_CHECK("k_spmm_stream");
+      return BLAST_OK;
+    };
+    if constexpr (C::PAIR)
+      return a.y_pairs && epi.pairs && !(B == 128 && !a.y_bf16) ? launch(std::true_type{}) : launch(std::false_type{});
+    else
+      return launch(std::true_type{});
+  } else {
   if constexpr (LONG) {
     sa.hdr1 = plan.hdr1;
     sa.chunk_row1 = plan.chunk_row1;
@@ -238,7 +257,7 @@ int launch_stream_tw(TileArgs a, const ChunkPlan& plan, int64_t k_features, hipS
     constexpr auto kernel = &k_spmm_stream<B, DUAL, TW, CHUNK, post.value, NW, LONG, false, pairs.value>;
     static blast::DeviceFlags lds_set;
     if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(kernel), C::LDS_BYTES, lds_set)) return rc;
-    kernel<<<dim3((unsigned)grid), dim3(64 * NW), C::LDS_BYTES, stream>>>(sa);
+    kernel<<<dim3((unsigned)grid), dim3(64 * NW), C::LDS_BYTES, stream>>>(sa, NoEpilogue{});
     BLAST_LAUNCH_CHECK("k_spmm_stream");
     return BLAST_OK;
   };
@@ -261,10 +280,11 @@ int launch_stream_tw(TileArgs a, const ChunkPlan& plan, int64_t k_features, hipS
     BLAST_LAUNCH_CHECK("k_long_finish");
   }
   return BLAST_OK;
+  }
 }
 
-template <int B, bool DUAL, bool CHUNK>
-int launch_stream_c(const TileArgs& a, const ChunkPlan& plan, int64_t k_features, hipStream_t stream) {
+template <int B, bool DUAL, bool CHUNK, class EPI = NoEpilogue>
+int launch_stream_c(const TileArgs& a, const ChunkPlan& plan, int64_t k_features, hipStream_t stream, const EPI& epi = EPI{}) {
   if constexpr (B == 128) {
     // 256-token x 128-row tiles (eight waves, one workgroup per CU) once every CU gets at least two of them;
     // below that, 128-token tiles in four-wave workgroups, two per CU (8B-shaped down projection at 2048
@@ -272,22 +292,22 @@ int launch_stream_c(const TileArgs& a, const ChunkPlan& plan, int64_t k_features
     const int64_t n_rows = CHUNK ? plan.max_chunks : (int64_t)a.nbr;
     const int64_t wide_items = (int64_t)((a.T + 255) / 256) * n_rows;
     if (wide_items >= 2 * (int64_t)cu_count())
-      return launch_stream_tw<B, DUAL, 4, CHUNK, 8>(a, plan, k_features, stream);
-    return launch_stream_tw<B, DUAL, 2, CHUNK>(a, plan, k_features, stream);
+      return launch_stream_tw<B, DUAL, 4, CHUNK, 8, false>(a, plan, k_features, stream, epi);
+    return launch_stream_tw<B, DUAL, 2, CHUNK, 4, false>(a, plan, k_features, stream, epi);
   } else if constexpr (B == 64) {
     // 128-token tiles when 256-token tiles would leave workgroup slots empty
     const int64_t wide_items = (int64_t)((a.T + 255) / 256) * a.nbr;
     if (wide_items < (int64_t)cu_count() * 2)
-      return launch_stream_tw<B, DUAL, 2, CHUNK>(a, plan, k_features, stream);
-    return launch_stream_tw<B, DUAL, 4, CHUNK>(a, plan, k_features, stream);
+      return launch_stream_tw<B, DUAL, 2, CHUNK, 4, false>(a, plan, k_features, stream, epi);
+    return launch_stream_tw<B, DUAL, 4, CHUNK, 4, false>(a, plan, k_features, stream, epi);
   } else {
-    return launch_stream_tw<B, DUAL, 4, CHUNK>(a, plan, k_features, stream);
+    return launch_stream_tw<B, DUAL, 4, CHUNK, 4, false>(a, plan, k_features, stream, epi);
   }
 }
 
-template <int B, bool DUAL>
-int launch_stream(const TileArgs& a, const ChunkPlan& plan, int64_t k_features, hipStream_t stream) {
-  if constexpr (!DUAL) {
+template <int B, bool DUAL, class EPI>
+int launch_stream(const TileArgs& a, const ChunkPlan& plan, int64_t k_features, hipStream_t stream, const EPI& epi) {
+  if constexpr (!DUAL && !EPI::kOn) {
     // rows cut into chunks accumulate with fp32 atomics: only for fp32 output without an activation
     if (plan.hdr && plan.stream_narrow && !a.y_bf16 && a.act < 0) {
       ChunkPlan narrow{};
@@ -314,12 +334,12 @@ int launch_stream(const TileArgs& a, const ChunkPlan& plan, int64_t k_features, 
   }
   ChunkPlan side{};  // no chunks; only the side job travels on
   side.zero_job = plan.zero_job;
-  return launch_stream_c<B, DUAL, false>(a, side, k_features, stream);
+  return launch_stream_c<B, DUAL, false>(a, side, k_features, stream, epi);
 }
 
 // Few output tiles: a workgroup per (64 rows of a block row, 64 tokens), see kern_split.h.
-template <int B, int NWAVES>
-int launch_split(const TileArgs& a, hipStream_t stream) {
+template <int B, int NWAVES, class EPI>
+int launch_split(const TileArgs& a, hipStream_t stream, const EPI& epi) {
   using C = SplitCfg<B, NWAVES>;
   const int64_t units = (int64_t)a.nbr * C::SUB, groups = (a.T + C::SB - 1) / C::SB;
   const int64_t grid = split_workgroups(units, groups, cu_count());
@@ -327,17 +347,20 @@ int launch_split(const TileArgs& a, hipStream_t stream) {
   if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
   auto launch = [&](auto post) {
     static blast::DeviceFlags lds_set;
-    if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_split<B, post.value, NWAVES>), C::LDS_BYTES, lds_set)) return rc;
-    k_spmm_split<B, post.value, NWAVES><<<dim3((unsigned)grid), dim3(64 * C::NW), C::LDS_BYTES, stream>>>(
-        a, (int)units, (int)groups, split_stride_log2(units, groups, cu_count()));
+    if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_split<B, post.value, NWAVES, EPI>), C::LDS_BYTES, lds_set)) return rc;
+    k_spmm_split<B, post.value, NWAVES, EPI><<<dim3((unsigned)grid), dim3(64 * C::NW), C::LDS_BYTES, stream>>>(
+        a, (int)units, (int)groups, split_stride_log2(units, groups, cu_count()), epi);
     BLAST_LAUNCH_CHECK("k_spmm_split");
     return (int)BLAST_OK;
   };
-  return a.act >= 0 ? launch(std::true_type{}) : launch(std::false_type{});
+  if constexpr (EPI::kOn)
+    return launch(std::false_type{});
+  else
+    return a.act >= 0 ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
-template <int B, bool DUAL, int NTT, bool CHUNK, int XSMALL = 0>
-int launch_decode_ntt(const TileArgs& a, const ChunkPlan& plan, hipStream_t stream) {
+template <int B, bool DUAL, int NTT, bool CHUNK, int XSMALL, class EPI = NoEpilogue>
+int launch_decode_ntt(const TileArgs& a, const ChunkPlan& plan, hipStream_t stream, const EPI& epi = EPI{}) {
   DecArgs d{};
   d.m0 = a.m0;
   d.m1 = a.m1;
@@ -361,6 +384,7 @@ int launch_decode_ntt(const TileArgs& a, const ChunkPlan& plan, hipStream_t stre
   if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
   d.n_units = (int)units;
   d.groups = (int)groups;
+  using C = DecCfg<B, DUAL, NTT, XSMALL>;
   int64_t total = grid;
   if (plan.zero_job && plan.zero_job->hdr && !plan.zero_job->wide && plan.zero_job->max_chunks > 0 &&
       grid + plan.zero_job->max_chunks <= INT32_MAX) {
@@ -378,35 +402,36 @@ int launch_decode_ntt(const TileArgs& a, const ChunkPlan& plan, hipStream_t stre
     total = grid + z.max_chunks;
     z.done = true;
   }
-  using C = DecCfg<B, DUAL, NTT, XSMALL>;
-  if constexpr (!DUAL && !CHUNK) {
+  if constexpr (!DUAL && !CHUNK && !EPI::kOn) {
     if (a.act >= 0) {  // single matrix with an activation on the output
       static blast::DeviceFlags lds_set_post;
       if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_decode<B, false, NTT, false, XSMALL, true>),
                                     C::LDS_BYTES, lds_set_post))
         return rc;
-      k_decode<B, false, NTT, false, XSMALL, true><<<dim3((unsigned)total), dim3(256), C::LDS_BYTES, stream>>>(d);
+      k_decode<B, false, NTT, false, XSMALL, true><<<dim3((unsigned)total), dim3(256), C::LDS_BYTES, stream>>>(d, epi);
       BLAST_LAUNCH_CHECK("k_decode");
       return BLAST_OK;
     }
   }
   static blast::DeviceFlags lds_set;
-  if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_decode<B, DUAL, NTT, CHUNK, XSMALL>), C::LDS_BYTES,
+  if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_decode<B, DUAL, NTT, CHUNK, XSMALL, false, false, EPI>), C::LDS_BYTES,
                                 lds_set))
     return rc;
-  if (CHUNK && !(plan.pre_zeroed && !plan.zeroed_wide)) {
-    StreamArgs sa{a, 0, -1, 0, plan.hdr, plan.chunk_row, plan.chunk_kb, plan.chunk_ke};
-    k_zero_shared_rows<B><<<dim3((unsigned)plan.max_chunks, (unsigned)((a.T + 63) / 64)), dim3(256), 0, stream>>>(sa);
-    BLAST_LAUNCH_CHECK("k_zero_shared_rows");
+  if constexpr (CHUNK) {
+    if (!(plan.pre_zeroed && !plan.zeroed_wide)) {
+      StreamArgs sa{a, 0, -1, 0, plan.hdr, plan.chunk_row, plan.chunk_kb, plan.chunk_ke};
+      k_zero_shared_rows<B><<<dim3((unsigned)plan.max_chunks, (unsigned)((a.T + 63) / 64)), dim3(256), 0, stream>>>(sa);
+      BLAST_LAUNCH_CHECK("k_zero_shared_rows");
+    }
   }
-  k_decode<B, DUAL, NTT, CHUNK, XSMALL><<<dim3((unsigned)total), dim3(256), C::LDS_BYTES, stream>>>(d);
+  k_decode<B, DUAL, NTT, CHUNK, XSMALL, false, false, EPI><<<dim3((unsigned)total), dim3(256), C::LDS_BYTES, stream>>>(d, epi);
   BLAST_LAUNCH_CHECK("k_decode");
   return BLAST_OK;
 }
 
-template <int B, bool DUAL>
-int launch_decode(const TileArgs& a, const ChunkPlan& plan, hipStream_t stream) {
-  if constexpr (!DUAL) {
+template <int B, bool DUAL, class EPI>
+int launch_decode(const TileArgs& a, const ChunkPlan& plan, hipStream_t stream, const EPI& epi) {
+  if constexpr (!DUAL && !EPI::kOn) {
     // rows cut into chunks accumulate with fp32 atomics: only for fp32 output without an activation
     if (plan.hdr && !a.y_bf16 && a.act < 0) {
       if constexpr (B >= 64) {
@@ -415,22 +440,22 @@ int launch_decode(const TileArgs& a, const ChunkPlan& plan, hipStream_t stream) 
       if constexpr (B == 128) {
         if (a.T <= 8) return launch_decode_ntt<B, false, 1, true, 2>(a, plan, stream);
       }
-      if (a.T <= 16) return launch_decode_ntt<B, false, 1, true>(a, plan, stream);
-      return launch_decode_ntt<B, false, 2, true>(a, plan, stream);
+      if (a.T <= 16) return launch_decode_ntt<B, false, 1, true, 0>(a, plan, stream);
+      return launch_decode_ntt<B, false, 2, true, 0>(a, plan, stream);
     }
   }
   ChunkPlan side{};  // no chunks; only the side job travels on
   side.zero_job = plan.zero_job;
   // the smallest activation tile that holds T token rows: 512 / B rows, at b = 128 also twice that
   if constexpr (B >= 64) {
-    if (a.T <= 512 / B) return launch_decode_ntt<B, DUAL, 1, false, 1>(a, side, stream);
+    if (a.T <= 512 / B) return launch_decode_ntt<B, DUAL, 1, false, 1>(a, side, stream, epi);
   }
   if constexpr (B == 128) {
-    if (a.T <= 8) return launch_decode_ntt<B, DUAL, 1, false, 2>(a, side, stream);
+    if (a.T <= 8) return launch_decode_ntt<B, DUAL, 1, false, 2>(a, side, stream, epi);
   }
-  if (a.T <= 16) return launch_decode_ntt<B, DUAL, 1, false>(a, side, stream);
+  if (a.T <= 16) return launch_decode_ntt<B, DUAL, 1, false, 0>(a, side, stream, epi);
   // groups of 32 tokens along gridDim.y (128-wide blocks: with a single activation tile per wave, see DecCfg)
-  return launch_decode_ntt<B, DUAL, 2, false>(a, side, stream);
+  return launch_decode_ntt<B, DUAL, 2, false, 0>(a, side, stream, epi);
 }
 
 // Crossover with the streaming kernel, from token sweeps on the 1B-shaped MLP.  The decode kernel
@@ -471,9 +496,9 @@ bool decode_applies(int b, const TileArgs& a, int64_t nnz, int64_t max_row_block
   return reread <= kDecodeMaxRereadBytes;
 }
 
-template <bool DUAL>
+template <bool DUAL, class EPI = NoEpilogue>
 int dispatch_tile(int b, const TileArgs& a, int64_t nnz, hipStream_t stream, const ChunkPlan& plan = ChunkPlan{},
-                  bool ranged = false) {
+                  bool ranged = false, const EPI& epi = EPI{}) {
   // the streaming kernel addresses activations with 32-bit byte offsets inside one column block
   const bool small_x = (int64_t)a.T * a.sxt * 2 < ((int64_t)1 << 32);
   const bool decode = a.x_vec && a.T > 0 && small_x && decode_applies<DUAL>(b, a, nnz, plan.max_row_blocks);
@@ -483,8 +508,8 @@ int dispatch_tile(int b, const TileArgs& a, int64_t nnz, hipStream_t stream, con
     const bool chunks = plan.hdr && !a.y_bf16 && a.act < 0;
     if (a.x_vec && small_x && !ranged && !chunks && !plan.zero_job) {
       const int waves = a.T > kDecodeAlwaysTokens ? split_waves(b, a.nbr, a.T, nnz, plan.fullest, decode, cu_count()) : 0;
-      if (waves == 4) return b == 64 ? launch_split<64, 4>(a, stream) : launch_split<128, 4>(a, stream);
-      if (waves == 8) return b == 64 ? launch_split<64, 8>(a, stream) : launch_split<128, 8>(a, stream);
+      if (waves == 4) return b == 64 ? launch_split<64, 4>(a, stream, epi) : launch_split<128, 4>(a, stream, epi);
+      if (waves == 8) return b == 64 ? launch_split<64, 8>(a, stream, epi) : launch_split<128, 8>(a, stream, epi);
     }
   }
   if (decode) {
@@ -503,9 +528,9 @@ int dispatch_tile(int b, const TileArgs& a, int64_t nnz, hipStream_t stream, con
       }
     }
     switch (b) {
-      case 32: return launch_decode<32, DUAL>(a, dplan, stream);
-      case 64: return launch_decode<64, DUAL>(a, dplan, stream);
-      case 128: return launch_decode<128, DUAL>(a, dplan, stream);
+      case 32: return launch_decode<32, DUAL>(a, dplan, stream, epi);
+      case 64: return launch_decode<64, DUAL>(a, dplan, stream, epi);
+      case 128: return launch_decode<128, DUAL>(a, dplan, stream, epi);
       default: break;
     }
   }
@@ -519,25 +544,25 @@ int dispatch_tile(int b, const TileArgs& a, int64_t nnz, hipStream_t stream, con
         part.T = (int)((a.T - t0 < range) ? a.T - t0 : range);
         part.X = a.X + t0 * a.sxt;
         part.Y = static_cast<char*>(a.Y) + t0 * a.syt * (a.y_bf16 ? 2 : 4);
-        if (int rc = dispatch_tile<DUAL>(b, part, nnz, stream, plan, true)) return rc;
+        if (int rc = dispatch_tile<DUAL>(b, part, nnz, stream, plan, true, epi.from(t0))) return rc;
       }
       return BLAST_OK;
     }
   }
   if (a.x_vec && a.T > 0 && small_x) {
     switch (b) {
-      case 32: return launch_stream<32, DUAL>(a, plan, a.kdim, stream);
-      case 64: return launch_stream<64, DUAL>(a, plan, a.kdim, stream);
-      case 128: return launch_stream<128, DUAL>(a, plan, a.kdim, stream);
+      case 32: return launch_stream<32, DUAL>(a, plan, a.kdim, stream, epi);
+      case 64: return launch_stream<64, DUAL>(a, plan, a.kdim, stream, epi);
+      case 128: return launch_stream<128, DUAL>(a, plan, a.kdim, stream, epi);
       default: break;
     }
   }
-  if (b == 16 && (a.x_vec || a.x_grp16) && a.T > 0) return launch_b16<DUAL>(a, nnz, stream);
+  if (b == 16 && (a.x_vec || a.x_grp16) && a.T > 0) return launch_b16<DUAL>(a, nnz, stream, epi);
   switch (b) {
-    case 16: return launch_tile<16, DUAL>(a, stream);
-    case 32: return launch_tile<32, DUAL>(a, stream);
-    case 64: return launch_tile<64, DUAL>(a, stream);
-    case 128: return launch_tile<128, DUAL>(a, stream);
+    case 16: return launch_tile<16, DUAL>(a, stream, epi);
+    case 32: return launch_tile<32, DUAL>(a, stream, epi);
+    case 64: return launch_tile<64, DUAL>(a, stream, epi);
+    case 128: return launch_tile<128, DUAL>(a, stream, epi);
     default: return BLAST_ERR_UNSUPPORTED_BLOCK;
   }
 }
