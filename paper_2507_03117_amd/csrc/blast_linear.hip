@@ -6,8 +6,8 @@ namespace {
 
 // 32-bit offsets inside a tile's 256 rows, as y_fast.
 bool rows_near(const void* p, int64_t ld) { return !p || (int64_t)257 * ld * 4 < ((int64_t)1 << 31); }
-bool rows_paired(const void* p, int64_t ld, int64_t value_bytes) {
-  return !p || (ld % 2 == 0 && blast::aligned(p, 2 * (size_t)value_bytes));
+bool rows_together(int n, const void* p, int64_t ld, int64_t value_bytes) {
+  return !p || (ld % n == 0 && blast::aligned(p, (size_t)(n * value_bytes)));
 }
 
 }  // namespace
@@ -49,7 +49,8 @@ extern "C" int blast_bsr_linear(const blast_bsr_view* W, const uint16_t* X, int6
   } else {
     e.srt = 1, e.sri = ldr, e.szt = 1, e.szi = ldz;
   }
-  e.pairs = rows_paired(R, ldr, e.r_bf16 ? 2 : 4) && rows_paired(Z, ldz, 2);
+  e.pairs = rows_together(2, R, ldr, e.r_bf16 ? 2 : 4) && rows_together(2, Z, ldz, 2);
+  e.quads = rows_together(4, R, ldr, e.r_bf16 ? 2 : 4) && rows_together(4, Z, ldz, 2);
   // feature-major operands, and pitches beyond 32-bit offsets, take the generic kernel
   if (layout != BLAST_TOKEN_MAJOR || !a.y_fast || !rows_near(R, ldr) || !rows_near(Z, ldz)) {
     switch (W->b) {

@@ -255,13 +255,22 @@ __global__ __launch_bounds__(NW * 64, DEPTH ? 4 : 1) void k_spmm_b16(const TileA
 
   // Result layout of the 16x16 instruction: lane -> token lane % 16, register j -> row 4 * (lane / 16) + j.
   const int64_t row0 = (int64_t)r * 16 + (lane >> 4) * 4;
+  EpilogueRows<4> rows[EPI::kOn ? NS : 1];
+  if constexpr (EPI::kOn) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int t = t0 + s * 16 + (lane & 15);
+      epilogue_load<4>(epi, rows[s], t < a.T ? t : a.T - 1, row0, epi.quads);
+    }
+  }
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
     const int t = t0 + s * 16 + (lane & 15);
     if (t >= a.T) continue;
     if constexpr (EPI::kOn) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc0[s][j] = epilogue_value(epi, acc0[s][j], t, row0 + j);
+      float v[4] = {acc0[s][0], acc0[s][1], acc0[s][2], acc0[s][3]};
+      epilogue_apply<4>(epi, rows[s], v, t, row0, epi.quads);
+      acc0[s] = f32x4_b16{v[0], v[1], v[2], v[3]};
     }
     if (y_vec) {
       const int64_t off = a.y_grp16 ? ((int64_t)r * a.T + t) * 16 + (lane >> 4) * 4 : (int64_t)t * a.syt + row0;

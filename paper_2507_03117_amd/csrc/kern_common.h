@@ -49,7 +49,7 @@ struct Epilogue {
   int64_t szt, szi;
   int r_bf16;
   int act;             // BLAST_ACT_*
-  int pairs;           // two neighbouring rows of a token of R and of Z may be read / stored as one value
+  int pairs, quads;    // two, four neighbouring rows of a token of R and of Z may be read / stored as one value
   // the same for the tokens from t0 on
   Epilogue from(int64_t t0) const {
     Epilogue e = *this;
@@ -137,7 +137,87 @@ __device__ __forceinline__ float apply_act(int act, float g) {
 
 __device__ __forceinline__ float bf16_value(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
-// One value through the epilogue: the kernels that end with a few values a lane.  `row` counts in the whole matrix.
+// N neighbouring rows' values (N = 1, 2, 4) of one token's residual and of the bias, asked for before they are needed: rows are
+// contiguous; `wide`: the address is aligned to the N values.
+template <int N>
+struct EpilogueRows {
+  uint32_t r[N];
+  float bias[N];
+};
+template <int N>
+__device__ __forceinline__ void epilogue_load(const Epilogue& e, EpilogueRows<N>& q, int64_t tok, int64_t row, bool wide) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    q.r[i] = 0;
+    q.bias[i] = 0.0f;
+  }
+  if (e.bias) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) q.bias[i] = e.bias[row + i];
+  }
+  if (e.R) {
+    typedef uint32_t Words __attribute__((ext_vector_type(N < 2 ? 2 : N)));
+    const int64_t at = tok * e.srt + row;
+    if (e.r_bf16) {
+      const uint16_t* p = static_cast<const uint16_t*>(e.R) + at;
+      if (N > 1 && wide) {  // taken apart when they are used, or the load would be waited for here
+        typedef uint32_t Pairs __attribute__((ext_vector_type(N < 4 ? 1 : N / 2)));
+        const Pairs w = *reinterpret_cast<const Pairs*>(p);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) q.r[i] = w[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) q.r[i] = p[i];
+      }
+    } else {
+      const uint32_t* p = static_cast<const uint32_t*>(e.R) + at;
+      if (N > 1 && wide) {
+        const Words w = *reinterpret_cast<const Words*>(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) q.r[i] = w[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) q.r[i] = p[i];
+      }
+    }
+  }
+}
+// The sums of those rows through the epilogue.
+template <int N>
+__device__ __forceinline__ void epilogue_apply(const Epilogue& e, const EpilogueRows<N>& q, float (&v)[N], int64_t tok, int64_t row, bool wide) {
+  if (e.bias) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += q.bias[i];
+  }
+  if (e.Z) {
+    uint16_t* p = e.Z + tok * e.szt + row;
+    typedef uint16_t Halves __attribute__((ext_vector_type(N < 2 ? 2 : N)));
+    if (N > 1 && wide) {
+      Halves h;
+#pragma unroll
+      for (int i = 0; i < N; ++i) h[i] = f32_to_bf16_rne(v[i]);
+      *reinterpret_cast<Halves*>(p) = h;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = f32_to_bf16_rne(v[i]);
+    }
+  }
+  if (e.act >= 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = post_act(e.act, v[i]);
+  }
+  if (e.R) {
+    if (N > 1 && e.r_bf16 && wide) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __uint_as_float(i % 2 ? q.r[i / 2] & 0xFFFF0000u : q.r[i / 2] << 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __uint_as_float(e.r_bf16 ? q.r[i] << 16 : q.r[i]);
+    }
+  }
+}
+
+// One value through the epilogue, in the generic kernel.  `row` counts in the whole matrix.
 __device__ __forceinline__ float epilogue_value(const Epilogue& e, float v, int64_t tok, int64_t row) {
   if (e.bias) v += e.bias[row];
   if (e.Z) e.Z[tok * e.szt + row * e.szi] = f32_to_bf16_rne(v);

@@ -639,6 +639,16 @@ __device__ __forceinline__ void decode_unit(const DecArgs& a, const int unit, co
 #pragma unroll
         for (int j = 0; j < 4; ++j) red[wave - 1][m][tt][j][lane] = acc[m][tt][j];
   }
+  EpilogueRows<1> rows[EPI::kOn ? 4 * NTT : 1];
+  if constexpr (EPI::kOn) {  // on their way while the waves meet
+    if (wave == 0) {
+#pragma unroll
+      for (int i = 0; i < 4 * NTT; ++i) {
+        const int tok = t_base + (i / 4) * 16 + 4 * g + i % 4;
+        epilogue_load<1>(epi, rows[i], tok < a.T ? tok : a.T - 1, (int64_t)r * B + q * 16 + l16, false);
+      }
+    }
+  }
   __syncthreads();
   if (wave > 0) return;
 #pragma unroll
@@ -662,7 +672,11 @@ __device__ __forceinline__ void decode_unit(const DecArgs& a, const int unit, co
         float v = acc[0][tt][j];
         if (DUAL) v = apply_act(a.act, v) * acc[NM - 1][tt][j];
         if (POST) v = apply_act(a.act, v);
-        if constexpr (EPI::kOn) v = epilogue_value(epi, v, tok, row);
+        if constexpr (EPI::kOn) {
+          float one[1] = {v};
+          epilogue_apply<1>(epi, rows[tt * 4 + j], one, tok, row, false);
+          v = one[0];
+        }
         const int64_t off = (int64_t)tok * a.syt + row * a.syi;
         if (TAGGED) {  // value and tag in one word: whoever sees the tag has the value
           if (!a.withhold)

@@ -145,10 +145,18 @@ __global__ __launch_bounds__(64 * NWAVES, 2) void k_spmm_split(const TileArgs a,
     for (int nj = 0; nj < 2; ++nj)
 #pragma unroll
       for (int v = 0; v < 16; ++v) red[wave][(mh * 2 + nj) * 16 + v][lane] = acc[0][mh][nj][v];
-  __syncthreads();
   constexpr int PER = 32 / C::NW;  // registers of a lane's half of the tile (token half, v) that a wave owns
   const int mi = wave * PER / 16, v0 = wave * PER % 16;
   const int64_t row = (int64_t)r * B + si * C::SB + 2 * l32;
+  EpilogueRows<2> rows[EPI::kOn ? PER : 1];
+  if constexpr (EPI::kOn) {  // on their way while the waves meet
+#pragma unroll
+    for (int v = 0; v < PER; ++v) {
+      const int t = t0 + 32 * mi + 2 * v0 + 8 * (v / 4) + 4 * lh + v % 4;
+      epilogue_load<2>(epi, rows[v], t < a.T ? t : a.T - 1, row, epi.pairs);
+    }
+  }
+  __syncthreads();
 #pragma unroll
   for (int v = 0; v < PER; ++v) {
     // register v0 + v of a 32 x 32 tile: token 8 * ((v0 + v) / 4) + 4 * lh + v % 4
@@ -164,8 +172,8 @@ __global__ __launch_bounds__(64 * NWAVES, 2) void k_spmm_split(const TileArgs a,
       auto pair = [&](int w) { return C::SETS == 2 ? part[w] : part[w] + part[(w + 4) % C::NW]; };
       const float sum = ((pair(0) + pair(1)) + pair(2)) + pair(3);
       y[nj] = POST ? post_act(a.act, sum) : sum;
-      if constexpr (EPI::kOn) y[nj] = epilogue_value(epi, sum, t, row + nj);
     }
+    if constexpr (EPI::kOn) epilogue_apply<2>(epi, rows[v], y, t, row, epi.pairs);
     const int64_t off = (int64_t)t * a.syt + row * a.syi;
     typedef __bf16 Bf16Pair __attribute__((ext_vector_type(2)));
     typedef float F32Pair __attribute__((ext_vector_type(2)));
