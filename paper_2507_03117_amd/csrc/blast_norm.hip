@@ -77,18 +77,27 @@ int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
   return launch_forward<16, 4, true>(a, stream);
 }
 
-// Workgroups that go over the rows of a backward pass, each with column sums of its own: one per CU.  From the token count
-// alone, so that the workspace does not depend on the device.
-constexpr int kBackwardGroups = 256;
-int64_t backward_groups(int64_t T, int rows) {
-  const int64_t n = (T + rows - 1) / rows;
-  return n < kBackwardGroups ? n : kBackwardGroups;
-}
+// Workgroups of a backward pass, each with column sums of its own: one to a row up to kBackwardRows rows, beyond that one of
+// sixteen waves per CU of the full card.  From the sizes alone, so that the workspace does not depend on the device.
+constexpr int kBackwardRows = 512, kBackwardGroups = 256;
 
-template <int NW, int NCH, bool VEC, bool LAYER, int MODE>
+template <int NW, int NCH, int TEAMS, bool VEC, bool LAYER, int MODE, int NL, bool LOW>
 int launch_backward_m(const NormArgs& a, hipStream_t stream) {
-  const int64_t grid = backward_groups(a.T, NW == 1 ? 4 : 1);
-  k_norm_backward<NW, NCH, VEC, LAYER, MODE><<<dim3((unsigned)grid), dim3(NW == 1 ? 256 : 64 * NW), 0, stream>>>(a);
+  constexpr int kThreads = 64 * NW * TEAMS;
+  constexpr size_t kLds = (TEAMS > 1 ? (size_t)kThreads : (size_t)NL * 64 * NW) * NCH * 8 * 4;
+  const int64_t rows = (a.T + TEAMS - 1) / TEAMS;
+  const int64_t grid = TEAMS == 1 && a.T <= kBackwardRows ? a.T : rows < kBackwardGroups ? rows : kBackwardGroups;
+  constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, LOW>;
+  if constexpr (kLds > 48 * 1024) {
+    static blast::DeviceFlags lds_set;
+    int dev = 0;
+    BLAST_HIP_TRY(hipGetDevice(&dev));
+    if (!lds_set.test(dev)) {
+      BLAST_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
+      lds_set.set(dev);
+    }
+  }
+  kernel<<<dim3((unsigned)grid), dim3(kThreads), kLds, stream>>>(a);
   BLAST_LAUNCH_CHECK("k_norm_backward");
   if (grid == 1) return BLAST_OK;
   JoinArgs j{};
@@ -104,28 +113,31 @@ int launch_backward_m(const NormArgs& a, hipStream_t stream) {
   return BLAST_OK;
 }
 
-template <int NW, int NCH, bool VEC>
+template <int NW, int NCH, int TEAMS, bool VEC, int NL = 0, bool LOW = false>
 int launch_backward(const NormArgs& a, hipStream_t stream) {
   const int mode = !a.y ? 0 : a.post ? 2 : 1;
   if (a.layer) {
-    if (mode == 0) return launch_backward_m<NW, NCH, VEC, true, 0>(a, stream);
-    if (mode == 1) return launch_backward_m<NW, NCH, VEC, true, 1>(a, stream);
-    return launch_backward_m<NW, NCH, VEC, true, 2>(a, stream);
+    if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, true, 0, NL, LOW>(a, stream);
+    if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, true, 1, NL, LOW>(a, stream);
+    return launch_backward_m<NW, NCH, TEAMS, VEC, true, 2, NL, LOW>(a, stream);
   }
-  if (mode == 0) return launch_backward_m<NW, NCH, VEC, false, 0>(a, stream);
-  if (mode == 1) return launch_backward_m<NW, NCH, VEC, false, 1>(a, stream);
-  return launch_backward_m<NW, NCH, VEC, false, 2>(a, stream);
+  if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, false, 0, NL, LOW>(a, stream);
+  if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, false, 1, NL, LOW>(a, stream);
+  return launch_backward_m<NW, NCH, TEAMS, VEC, false, 2, NL, LOW>(a, stream);
 }
 
 int dispatch_backward(const NormArgs& a, bool vec, hipStream_t stream) {
-  if (!vec) return a.width <= 2048 ? launch_backward<4, 1, false>(a, stream) : launch_backward<16, 4, false>(a, stream);
-  if (a.width <= 512) return launch_backward<1, 1, true>(a, stream);
-  if (a.width <= 1024) return launch_backward<1, 2, true>(a, stream);
-  if (a.width <= 2048) return launch_backward<4, 1, true>(a, stream);
-  if (a.width <= 4096) return launch_backward<8, 1, true>(a, stream);
-  if (a.width <= 8192) return launch_backward<16, 1, true>(a, stream);
-  if (a.width <= 16384) return launch_backward<16, 2, true>(a, stream);
-  return launch_backward<16, 4, true>(a, stream);
+  if (!vec) return a.width <= 2048 ? launch_backward<4, 1, 1, false>(a, stream) : launch_backward<16, 4, 1, false>(a, stream);
+  const bool few = a.T <= kBackwardRows;
+  const bool low = a.h_bf16 && a.dx_bf16 && (!a.w || a.p_bf16) &&
+                   (!a.y || (a.y_bf16 && (!a.dy || a.dy_bf16) && (!a.gate || a.g_bf16) && ((!a.pw && !a.pb) || a.p_bf16)));
+  if (a.width <= 512) return few ? launch_backward<1, 1, 1, true>(a, stream) : launch_backward<1, 1, 16, true>(a, stream);
+  if (a.width <= 1024) return few ? launch_backward<2, 1, 1, true>(a, stream) : launch_backward<2, 1, 8, true>(a, stream);
+  if (a.width <= 2048) return few ? launch_backward<4, 1, 1, true>(a, stream) : launch_backward<4, 1, 4, true>(a, stream);
+  if (a.width <= 4096) return few ? launch_backward<8, 1, 1, true>(a, stream) : launch_backward<8, 1, 2, true>(a, stream);
+  if (a.width <= 8192) return launch_backward<16, 1, 1, true>(a, stream);
+  if (a.width <= 16384) return low ? launch_backward<16, 2, 1, true, 2, true>(a, stream) : launch_backward<16, 2, 1, true, 2>(a, stream);
+  return launch_backward<16, 4, 1, true>(a, stream);
 }
 
 }  // namespace
@@ -168,7 +180,7 @@ extern "C" int blast_norm_residual_backward_workspace(const blast_norm_view* P, 
   if (T < 0 || T > INT32_MAX / 2 || !ws_bytes) return BLAST_ERR_INVALID_ARG;
   const int layer = P->kind == BLAST_NORM_LAYER;
   const int sums = 1 + layer + (P->post ? 1 + layer : 0) + (P->gate && P->ldg == 0 ? 1 : 0);
-  *ws_bytes = T <= 1 ? 0 : (size_t)sums * (size_t)backward_groups(T, 1) * (size_t)P->width * 4;
+  *ws_bytes = T <= 1 ? 0 : (size_t)sums * (size_t)(T < kBackwardRows ? T : kBackwardRows) * (size_t)P->width * 4;
   return BLAST_OK;
 }
 

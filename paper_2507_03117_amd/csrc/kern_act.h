@@ -54,9 +54,9 @@ __global__ __launch_bounds__(256) void k_act_backward(const ActArgs a) {
   for (int j = 0; j < 8; ++j) sum[0][j] = sum[1][j] = 0.0f;
   for (int t = run * a.run + team; t < t_end; t += kActTeams) {
     Piece z{}, u{}, dy{};
-    if (a.z) piece_load<32, VEC>(z, a.z, t * a.ldz + col0, 0, lane, width, 1);
-    if (GATED) piece_load<32, VEC>(u, a.u, t * a.ldu + col0, 0, lane, width, 1);
-    piece_load<32, VEC>(dy, a.dy, t * a.lddy + col0, 0, lane, width, a.dy_bf16);
+    if (a.z) piece_load<32, VEC>(z, row_of(a.z, t * a.ldz + col0, 1), 0, lane, width, 1);
+    if (GATED) piece_load<32, VEC>(u, row_of(a.u, t * a.ldu + col0, 1), 0, lane, width, 1);
+    piece_load<32, VEC>(dy, row_of(a.dy, t * a.lddy + col0, a.dy_bf16), 0, lane, width, a.dy_bf16);
     float zv[8], uv[8], d[8], av[8], dz[8], du[8];
     piece_values<VEC>(z, 1, zv);
     piece_values<VEC>(dy, a.dy_bf16, d);
@@ -73,10 +73,10 @@ __global__ __launch_bounds__(256) void k_act_backward(const ActArgs a) {
         if (SUMS) sum[1][j] += du[j];
       }
     }
-    if (a.dz) piece_store<32, VEC>(a.dz, t * a.lddz + col0, 0, lane, width, 1, dz);
+    if (a.dz) piece_store<32, VEC>(row_of(a.dz, t * a.lddz + col0, 1), 0, lane, width, 1, dz);
     if (GATED) {
-      if (a.du) piece_store<32, VEC>(a.du, t * a.lddu + col0, 0, lane, width, 1, du);
-      if (a.h) piece_store<32, VEC>(a.h, t * a.ldh + col0, 0, lane, width, 1, av);
+      if (a.du) piece_store<32, VEC>(row_of(a.du, t * a.lddu + col0, 1), 0, lane, width, 1, du);
+      if (a.h) piece_store<32, VEC>(row_of(a.h, t * a.ldh + col0, 1), 0, lane, width, 1, av);
     }
   }
   if constexpr (SUMS) {

@@ -8,8 +8,9 @@ namespace blast_dev {
 // Eight values of a row as they lie in memory: bf16 pairs in the first four words or fp32 values; with element-wise access
 // one value a word.  They are converted only when they are used: loads of several tensors are then all on their way before
 // the first is waited for, whatever their types (the types are the same for all lanes: the branches are scalar).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 struct Piece {
-  uint32_t v[8];
+  u32x4 lo, hi;
 };
 
 // Element j of piece c of lane `lane` of the NT lanes that share a row: VEC keeps a lane's eight together, so that a lane
@@ -19,42 +20,56 @@ __device__ __forceinline__ int piece_at(int c, int j, int lane) {
   return VEC ? (c * NT + lane) * 8 + j : (c * 8 + j) * NT + lane;
 }
 
+// A row of a tensor: the same for all lanes that share it, so that an access is a scalar base and a lane's 32-bit offset.
+__device__ __forceinline__ const unsigned char* row_of(const void* base, int64_t at, int bf16) {
+  return static_cast<const unsigned char*>(base) + (bf16 ? at * 2 : at * 4);
+}
+__device__ __forceinline__ unsigned char* row_of(void* base, int64_t at, int bf16) {
+  return static_cast<unsigned char*>(base) + (bf16 ? at * 2 : at * 4);
+}
+
+// Four values that are the same for all lanes and that the launch does not write, through the scalar unit.
+__device__ __forceinline__ float4 scalar_float4(const float* p) {
+  const auto* q = reinterpret_cast<const __attribute__((address_space(4))) float*>(reinterpret_cast<uintptr_t>(p));
+  return float4{q[0], q[1], q[2], q[3]};
+}
+
 template <int NT, bool VEC>
-__device__ __forceinline__ void piece_load(Piece& q, const void* base, int64_t row, int c, int lane, int width, int bf16) {
+__device__ __forceinline__ void piece_load(Piece& q, const unsigned char* row, int c, int lane, int width, int bf16) {
   if constexpr (VEC) {
-    const int e = (c * NT + lane) * 8;
-    if (e < width) {
-      uint4 lo, hi;
+    const uint32_t e = (uint32_t)(c * NT + lane) * 8;
+    if (e < (uint32_t)width) {
       if (bf16) {
-        lo = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + row + e);
-        hi = uint4{0, 0, 0, 0};
+        q.lo = *reinterpret_cast<const u32x4*>(row + e * 2);
       } else {
-        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(base) + row + e);
-        lo = p[0];
-        hi = p[1];
+        const u32x4* p = reinterpret_cast<const u32x4*>(row + e * 4);
+        q.lo = p[0];
+        q.hi = p[1];
       }
-      q.v[0] = lo.x, q.v[1] = lo.y, q.v[2] = lo.z, q.v[3] = lo.w;
-      q.v[4] = hi.x, q.v[5] = hi.y, q.v[6] = hi.z, q.v[7] = hi.w;
     }
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int e = (c * 8 + j) * NT + lane;
-      if (e < width)
-        q.v[j] = bf16 ? static_cast<const uint16_t*>(base)[row + e] : static_cast<const uint32_t*>(base)[row + e];
+      const uint32_t e = (uint32_t)((c * 8 + j) * NT + lane);
+      uint32_t v = 0;
+      if (e < (uint32_t)width) v = bf16 ? *reinterpret_cast<const uint16_t*>(row + e * 2) : *reinterpret_cast<const uint32_t*>(row + e * 4);
+      if (j < 4)
+        q.lo[j & 3] = v;
+      else
+        q.hi[j & 3] = v;
     }
   }
 }
 
 template <bool VEC>
 __device__ __forceinline__ void piece_values(const Piece& q, int bf16, float (&out)[8]) {
+  auto word = [&](int i) { return i < 4 ? q.lo[i & 3] : q.hi[i & 3]; };
   if (bf16) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      out[j] = __uint_as_float(!VEC ? q.v[j] << 16 : j % 2 ? q.v[j / 2] & 0xFFFF0000u : q.v[j / 2] << 16);
+    for (int j = 0; j < 8; ++j) out[j] = __uint_as_float(!VEC ? word(j) << 16 : j % 2 ? word(j / 2) & 0xFFFF0000u : word(j / 2) << 16);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) out[j] = __uint_as_float(q.v[j]);
+    for (int j = 0; j < 8; ++j) out[j] = __uint_as_float(word(j));
   }
 }
 
@@ -63,15 +78,15 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 }
 
 template <int NT, bool VEC>
-__device__ __forceinline__ void piece_store(void* base, int64_t row, int c, int lane, int width, int bf16, const float (&v)[8]) {
+__device__ __forceinline__ void piece_store(unsigned char* row, int c, int lane, int width, int bf16, const float (&v)[8]) {
   if constexpr (VEC) {
-    const int e = (c * NT + lane) * 8;
-    if (e < width) {
+    const uint32_t e = (uint32_t)(c * NT + lane) * 8;
+    if (e < (uint32_t)width) {
       if (bf16) {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + row + e) =
-            uint4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+        *reinterpret_cast<u32x4*>(row + e * 2) =
+            u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
       } else {
-        float4* p = reinterpret_cast<float4*>(static_cast<float*>(base) + row + e);
+        float4* p = reinterpret_cast<float4*>(row + e * 4);
         p[0] = float4{v[0], v[1], v[2], v[3]};
         p[1] = float4{v[4], v[5], v[6], v[7]};
       }
@@ -79,12 +94,12 @@ __device__ __forceinline__ void piece_store(void* base, int64_t row, int c, int 
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int e = (c * 8 + j) * NT + lane;
-      if (e < width) {
+      const uint32_t e = (uint32_t)((c * 8 + j) * NT + lane);
+      if (e < (uint32_t)width) {
         if (bf16)
-          static_cast<uint16_t*>(base)[row + e] = f32_to_bf16_rne(v[j]);
+          *reinterpret_cast<uint16_t*>(row + e * 2) = f32_to_bf16_rne(v[j]);
         else
-          static_cast<float*>(base)[row + e] = v[j];
+          *reinterpret_cast<float*>(row + e * 4) = v[j];
       }
     }
   }
@@ -110,6 +125,7 @@ __device__ __forceinline__ float wave_sum(float x) {
 template <int NW>
 struct RowSum {
   float (*buf)[NW][2];
+  int wave;  // of the row's NW
   int turn = 0;
   template <int N>
   __device__ __forceinline__ void operator()(float (&s)[N]) {
@@ -117,7 +133,6 @@ struct RowSum {
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
     if constexpr (NW > 1) {
-      const int wave = threadIdx.x >> 6;
       if ((threadIdx.x & 63) == 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) buf[turn][wave][i] = s[i];
