@@ -618,15 +618,16 @@ def _rows_of(t: Optional[torch.Tensor], shape, dtypes):
     """(address, row pitch) of an operand of that shape with contiguous rows; (None, 0) without one."""
     if t is None:
         return None, 0
-    assert t.is_cuda and tuple(t.shape) == tuple(shape) and t.dtype in dtypes, (tuple(t.shape), t.dtype, shape)
-    assert t.shape[1] <= 1 or t.stride(1) == 1
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    ld, step = t.stride()
+    rows, cols = shape
+    assert t.is_cuda and t.shape == shape and t.dtype in dtypes and (step == 1 or cols <= 1), (t.shape, t.stride(), t.dtype, shape)
+    return t.data_ptr(), ld if rows > 1 or ld > cols else cols
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtypes):
     if t is None:
         return None
-    assert t.is_cuda and t.dim() == 1 and t.numel() == n and t.dtype in dtypes and (n <= 1 or t.stride(0) == 1)
+    assert t.is_cuda and t.shape == (n,) and t.dtype in dtypes and (n <= 1 or t.stride(0) == 1)
     return t.data_ptr()
 
 
@@ -697,29 +698,25 @@ class ActGrads:
 
 def _act_backward(Z, U, dY, act, dZ, dU, H, dbias_z, dbias_u):
     assert dY.dim() == 2
-    L, (T, N) = lib(), dY.shape
-    low, sums = (torch.bfloat16,), (torch.float32,)
-    operands = []
-    for t in (Z, U):
-        operands += _rows_of(t, (T, N), low)
-    operands += _rows_of(dY, (T, N), _EITHER)
-    results = []
-    for t in (dZ, dU, H):
-        results += _rows_of(t, (T, N), low)
-    wanted, ws, wsb = (dbias_z is not None) + (dbias_u is not None), None, C.c_size_t(0)
+    L, shape, low = lib(), dY.shape, (torch.bfloat16,)
+    T, N = shape
+    wanted, ws, ws_bytes = (dbias_z is not None) + (dbias_u is not None), None, 0
     if wanted:
+        wsb = C.c_size_t(0)
         _check(L.blast_act_backward_workspace(T, N, wanted, C.byref(wsb)), "blast_act_backward_workspace")
-        ws = torch.empty(wsb.value, dtype=torch.uint8, device=dY.device) if wsb.value else None
-    _check(L.blast_act_backward(*operands, _dtype_code(dY.dtype), T, N, ACT_NONE if act is None else ACT[act], *results,
-                                _vector(dbias_z, N, sums), _vector(dbias_u, N, sums), _ptr(ws), wsb.value, _stream()),
-           "blast_act_backward")
+        ws_bytes = wsb.value
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dY.device) if ws_bytes else None
+    _check(L.blast_act_backward(*_rows_of(Z, shape, low), *_rows_of(U, shape, low), *_rows_of(dY, shape, _EITHER),
+                                _dtype_code(dY.dtype), T, N, ACT_NONE if act is None else ACT[act], *_rows_of(dZ, shape, low),
+                                *_rows_of(dU, shape, low), *_rows_of(H, shape, low), _ptr(dbias_z), _ptr(dbias_u), _ptr(ws),
+                                ws_bytes, _stream()), "blast_act_backward")
 
 
 def act_backward(Z: Optional[torch.Tensor], dY: torch.Tensor, *, act: Optional[str] = None, bias_grad: bool = False,
                  out: Optional[torch.Tensor] = None) -> ActGrads:
     """blast_act_backward of one matrix: dZ = dY * act'(Z) (bf16) and, with bias_grad, dbias = its sum over the tokens.
     Z: the `pre` of bsr_linear, bf16 [T, N]; None without an activation."""
-    dZ = out if out is not None else torch.empty(dY.shape, dtype=torch.bfloat16, device=dY.device)
+    dZ = out if out is not None else torch.empty_like(dY, dtype=torch.bfloat16)
     db = torch.empty(dY.shape[1], dtype=torch.float32, device=dY.device) if bias_grad else None
     _act_backward(Z, None, dY, act, dZ, None, None, db, None)
     return ActGrads(dZ=dZ, dbias=db)
@@ -729,38 +726,44 @@ def gated_act_backward(G: torch.Tensor, U: torch.Tensor, dH: torch.Tensor, *, ac
                        with_h: bool = True) -> ActGrads:
     """blast_act_backward of the gated product H = act(G) * U: dG, dU and (with_h) H again, bf16; with bias_grad the sums of dG
     and dU over the tokens."""
-    new = lambda: torch.empty(dH.shape, dtype=torch.bfloat16, device=dH.device)  # noqa: E731
-    col = lambda: torch.empty(dH.shape[1], dtype=torch.float32, device=dH.device) if bias_grad else None  # noqa: E731
-    g = ActGrads(dG=new(), dU=new(), H=new() if with_h else None, dbias_g=col(), dbias_u=col())
     assert U is not None
-    _act_backward(G, U, dH, act, g.dG, g.dU, g.H, g.dbias_g, g.dbias_u)
-    return g
+    dG, dU = torch.empty_like(dH, dtype=torch.bfloat16), torch.empty_like(dH, dtype=torch.bfloat16)
+    H = torch.empty_like(dH, dtype=torch.bfloat16) if with_h else None
+    dbg = dbu = None
+    if bias_grad:
+        dbg, dbu = (torch.empty(dH.shape[1], dtype=torch.float32, device=dH.device) for _ in range(2))
+    _act_backward(G, U, dH, act, dG, dU, H, dbg, dbu)
+    return ActGrads(None, None, dG, dU, H, dbg, dbu)
 
 
 def _norm_view(width, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps) -> NormView:
-    given = [p for p in (weight, bias, post_weight, post_bias) if p is not None]
-    dtype = given[0].dtype if given else torch.float32
-    assert all(p.dtype == dtype for p in given), "weights and biases have one type"
-    p = [_vector(t, width, (dtype,)) if t is not None else None for t in (weight, bias, post_weight, post_bias)]
-    g, ldg, g_dtype = None, 0, torch.float32
+    dtype, p = None, [None, None, None, None]
+    for i, t in enumerate((weight, bias, post_weight, post_bias)):
+        if t is not None:
+            if dtype is None:
+                dtype = t.dtype
+            assert dtype in _EITHER, "fp32 or bf16"
+            p[i] = _vector(t, width, (dtype,))  # (weights and biases have one type)
+    g, ldg, g_dtype = None, 0, None
     if gate is not None:
         g_dtype = gate.dtype
         if gate.dim() == 1:
             g = _vector(gate, width, _EITHER)
         else:
             g, ldg = _rows_of(gate, (T, width), _EITHER)
-    return NormView(width, NORM[kind], 1 if post else 0, eps, scale, _dtype_code(dtype), _dtype_code(g_dtype), *p, g, ldg)
+    return NormView(width, NORM[kind], 1 if post else 0, eps, scale, BF16 if dtype == torch.bfloat16 else F32,
+                    BF16 if g_dtype == torch.bfloat16 else F32, p[0], p[1], p[2], p[3], g, ldg)
 
 
 def _norm_args(h, y, h_out, x, stats):
-    assert h.dim() == 2
-    T, E = h.shape
-    hp, ldh = _rows_of(h, (T, E), _EITHER)
-    yp, ldy = _rows_of(y, (T, E), _EITHER)
-    op, ldo = (None, 0) if y is None else _rows_of(h_out, (T, E), (h.dtype,))
-    xp, ldx = _rows_of(x, (T, E), _EITHER)
+    shape = h.shape
+    T, _ = shape
+    hp, ldh = _rows_of(h, shape, _EITHER)
+    yp, ldy = _rows_of(y, shape, _EITHER)
+    op, ldo = (None, 0) if y is None else _rows_of(h_out, shape, (h.dtype,))
+    xp, ldx = _rows_of(x, shape, _EITHER)
     if stats is not None:
-        assert stats.is_cuda and stats.dtype == torch.float32 and tuple(stats.shape) == (T, 4) and stats.is_contiguous()
+        assert stats.is_cuda and stats.dtype == torch.float32 and stats.shape == (T, 4) and stats.is_contiguous()
     return (hp, ldh, _dtype_code(h.dtype), yp, ldy, F32 if y is None else _dtype_code(y.dtype), T, op, ldo, xp, ldx,
             _dtype_code(x.dtype), _ptr(stats))
 
@@ -773,11 +776,13 @@ def norm_residual(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, kind: st
                   out: Optional[torch.Tensor] = None, with_stats: bool = False):
     """blast_norm_residual: h' = h + scale * gate * (post-)norm(y) and x = norm(h') * weight + bias; returns (h', x), with
     with_stats (h', x, stats).  Without y: x = norm(h) and h' is h.  gate: [width] or [T, width]; h_out may be h."""
-    new_h = h if y is None else h_out if h_out is not None else torch.empty(h.shape, dtype=h.dtype, device=h.device)
-    x = out if out is not None else torch.empty(h.shape, dtype=out_dtype, device=h.device)
-    stats = torch.empty((h.shape[0], 4), dtype=torch.float32, device=h.device) if with_stats else None
-    v = _norm_view(h.shape[1], h.shape[0], kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
-    _check(lib().blast_norm_residual(C.byref(v), *_norm_args(h, y, new_h, x, stats), _stream()), "blast_norm_residual")
+    assert h.dim() == 2
+    T, E = h.shape
+    new_h = h if y is None else h_out if h_out is not None else torch.empty_like(h)
+    x = out if out is not None else torch.empty_like(h, dtype=out_dtype)
+    stats = torch.empty((T, 4), dtype=torch.float32, device=h.device) if with_stats else None
+    v = _norm_view(E, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
+    _check(lib().blast_norm_residual(v, *_norm_args(h, y, new_h, x, stats), _stream()), "blast_norm_residual")
     return (new_h, x, stats) if with_stats else (new_h, x)
 
 
@@ -819,30 +824,40 @@ def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats
     assert h_out.dim() == 2
     T, E = h_out.shape
     dev = h_out.device
+    shape, h_dtype = h_out.shape, h_out.dtype
     v = _norm_view(E, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
-    col = lambda given: torch.empty(E, dtype=torch.float32, device=dev) if given is not None else None  # noqa: E731
-    branch = y is not None
-    g = NormGrads(dh=dh if dh is not None else torch.empty((T, E), dtype=h_out.dtype, device=dev),
-                  dy=torch.empty((T, E), dtype=dy_dtype, device=dev) if branch else None, dgate=None, dweight=col(weight),
-                  dbias=col(bias), dpost_weight=col(post_weight) if branch and post else None,
-                  dpost_bias=col(post_bias) if branch and post else None)
-    if branch and gate is not None:
-        g.dgate = col(gate) if gate.dim() == 1 else torch.empty((T, E), dtype=gate.dtype, device=dev)
-    assert stats.is_cuda and stats.dtype == torch.float32 and tuple(stats.shape) == (T, 4) and stats.is_contiguous()
-    hp, ldh = _rows_of(h_out, (T, E), _EITHER)
-    yp, ldy = _rows_of(y, (T, E), _EITHER)
-    dxp, lddx = _rows_of(dx, (T, E), _EITHER)
-    dhop, lddho = _rows_of(dh_out, (T, E), (h_out.dtype,))
-    dhp, lddh = _rows_of(g.dh, (T, E), (h_out.dtype,))
-    dyp, lddy = _rows_of(g.dy, (T, E), _EITHER)
-    lddg = 0 if g.dgate is None or g.dgate.dim() == 1 else _rows_of(g.dgate, (T, E), _EITHER)[1]
+    branch, same = y is not None, (h_dtype,)
+    sums = {"dtype": torch.float32, "device": dev}
+    dh = dh if dh is not None else torch.empty_like(h_out)
+    dy = dgate = dpost_weight = dpost_bias = None
+    dyp, lddy, lddg = None, 0, 0
+    if branch:
+        dy = torch.empty_like(h_out, dtype=dy_dtype)
+        dyp, lddy = _rows_of(dy, shape, _EITHER)
+        if gate is not None:
+            if gate.dim() == 1:
+                dgate = torch.empty(E, **sums)
+            else:
+                dgate = torch.empty_like(gate)
+                lddg = _rows_of(dgate, shape, _EITHER)[1]
+        if post:
+            dpost_weight = None if post_weight is None else torch.empty(E, **sums)
+            dpost_bias = None if post_bias is None else torch.empty(E, **sums)
+    dweight = None if weight is None else torch.empty(E, **sums)
+    dbias = None if bias is None else torch.empty(E, **sums)
+    assert stats.is_cuda and stats.dtype == torch.float32 and stats.shape == (T, 4) and stats.is_contiguous()
+    hp, ldh = _rows_of(h_out, shape, _EITHER)
+    yp, ldy = _rows_of(y, shape, _EITHER)
+    dxp, lddx = _rows_of(dx, shape, _EITHER)
+    dhop, lddho = _rows_of(dh_out, shape, same)
+    dhp, lddh = _rows_of(dh, shape, same)
     wsb, ws = C.c_size_t(0), None
-    _check(L.blast_norm_residual_backward_workspace(C.byref(v), T, C.byref(wsb)), "blast_norm_residual_backward_workspace")
-    if wsb.value:
-        ws = torch.empty(wsb.value, dtype=torch.uint8, device=dev)
+    _check(L.blast_norm_residual_backward_workspace(v, T, C.byref(wsb)), "blast_norm_residual_backward_workspace")
+    ws_bytes = wsb.value
+    if ws_bytes:
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
     _check(L.blast_norm_residual_backward(
-        C.byref(v), hp, ldh, _dtype_code(h_out.dtype), yp, ldy, F32 if y is None else _dtype_code(y.dtype), stats.data_ptr(),
-        dxp, lddx, _dtype_code(dx.dtype), dhop, lddho, T, dhp, lddh, dyp, lddy, _dtype_code(dy_dtype), _ptr(g.dgate), lddg,
-        _ptr(g.dweight), _ptr(g.dbias), _ptr(g.dpost_weight), _ptr(g.dpost_bias), _ptr(ws), wsb.value, _stream()),
-        "blast_norm_residual_backward")
-    return g
+        v, hp, ldh, _dtype_code(h_dtype), yp, ldy, _dtype_code(y.dtype) if branch else F32, stats.data_ptr(), dxp, lddx,
+        _dtype_code(dx.dtype), dhop, lddho, T, dhp, lddh, dyp, lddy, _dtype_code(dy_dtype), _ptr(dgate), lddg, _ptr(dweight),
+        _ptr(dbias), _ptr(dpost_weight), _ptr(dpost_bias), _ptr(ws), ws_bytes, _stream()), "blast_norm_residual_backward")
+    return NormGrads(dh, dy, dgate, dweight, dbias, dpost_weight, dpost_bias)
