@@ -69,10 +69,10 @@ int launch_forward(const NormArgs& a, hipStream_t stream) {
 int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
   if (!vec) return a.width <= 2048 ? launch_forward<4, 1, false>(a, stream) : launch_forward<16, 4, false>(a, stream);
   if (a.width <= 512) return launch_forward<1, 1, true>(a, stream);
-  if (a.width <= 1024) return launch_forward<1, 2, true>(a, stream);
-  if (a.width <= 2048) return launch_forward<2, 2, true>(a, stream);
-  if (a.width <= 4096) return launch_forward<4, 2, true>(a, stream);
-  if (a.width <= 8192) return launch_forward<8, 2, true>(a, stream);
+  if (a.width <= 1024) return launch_forward<2, 1, true>(a, stream);
+  if (a.width <= 2048) return launch_forward<4, 1, true>(a, stream);
+  if (a.width <= 4096) return launch_forward<8, 1, true>(a, stream);
+  if (a.width <= 8192) return launch_forward<16, 1, true>(a, stream);
   if (a.width <= 16384) return launch_forward<16, 2, true>(a, stream);
   return launch_forward<16, 4, true>(a, stream);
 }

@@ -39,18 +39,13 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
   const int E = a.width;
   const float inv_e = 1.0f / (float)E;
   const bool branch = a.y != nullptr;
-  Piece h[NCH], y[NCH], g[NCH], w[NCH], b[NCH], pw[NCH], pb[NCH];
+  auto ask = [&](Piece (&q)[NCH], const void* p, int64_t at, int bf16) {
 #pragma unroll
-  for (int c = 0; c < NCH; ++c) {
-    h[c] = y[c] = g[c] = w[c] = b[c] = pw[c] = pb[c] = Piece{};
-    piece_load<NT, VEC>(h[c], row_of(a.h, t * a.ldh, a.h_bf16), c, lane, E, a.h_bf16);
-    if (branch) piece_load<NT, VEC>(y[c], row_of(a.y, t * a.ldy, a.y_bf16), c, lane, E, a.y_bf16);
-    if (a.gate) piece_load<NT, VEC>(g[c], row_of(a.gate, t * a.ldg, a.g_bf16), c, lane, E, a.g_bf16);
-    if (a.w) piece_load<NT, VEC>(w[c], row_of(a.w, 0, a.p_bf16), c, lane, E, a.p_bf16);
-    if (a.b) piece_load<NT, VEC>(b[c], row_of(a.b, 0, a.p_bf16), c, lane, E, a.p_bf16);
-    if (a.pw) piece_load<NT, VEC>(pw[c], row_of(a.pw, 0, a.p_bf16), c, lane, E, a.p_bf16);
-    if (a.pb) piece_load<NT, VEC>(pb[c], row_of(a.pb, 0, a.p_bf16), c, lane, E, a.p_bf16);
-  }
+    for (int c = 0; c < NCH; ++c) {
+      q[c] = Piece{};
+      if (p) piece_load<NT, VEC>(q[c], row_of(p, at, bf16), c, lane, E, bf16);
+    }
+  };
   auto inside = [&](int c, int j) { return piece_at<NT, VEC>(c, j, lane) < E; };
   // mean (0 without `layer`) and reciprocal deviation; v becomes the normalised values
   auto normalise = [&](float (&v)[NCH][8], float& mean, float& r) {
@@ -94,10 +89,15 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
     }
   };
   float v[NCH][8], st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int c = 0; c < NCH; ++c) piece_values<VEC>(h[c], a.h_bf16, v[c]);
+  Piece h[NCH], g[NCH], w[NCH], b[NCH];
   if (branch) {
+    Piece y[NCH], pw[NCH], pb[NCH];
     float p[NCH][8];
+    ask(y, a.y, t * a.ldy, a.y_bf16);
+    ask(h, a.h, t * a.ldh, a.h_bf16);
+    ask(g, a.gate, t * a.ldg, a.g_bf16);
+    ask(pw, a.pw, 0, a.p_bf16);
+    ask(pb, a.pb, 0, a.p_bf16);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) piece_values<VEC>(y[c], a.y_bf16, p[c]);
     if (a.post) {
@@ -107,6 +107,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
     }
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
+      piece_values<VEC>(h[c], a.h_bf16, v[c]);
       if (a.gate) {
         float f[8];
         piece_values<VEC>(g[c], a.g_bf16, f);
@@ -117,6 +118,15 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
       for (int j = 0; j < 8; ++j) v[c][j] = __builtin_fmaf(a.scale, p[c][j], v[c][j]);
       piece_store<NT, VEC>(row_of(a.h_out, t * a.ldho, a.h_bf16), c, lane, E, a.h_bf16, v[c]);
     }
+  } else {
+    ask(h, a.h, t * a.ldh, a.h_bf16);
+  }
+  // (in registers that the branch no longer needs; the row's sums take a while)
+  ask(w, a.w, 0, a.p_bf16);
+  ask(b, a.b, 0, a.p_bf16);
+  if (!branch) {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) piece_values<VEC>(h[c], a.h_bf16, v[c]);
   }
   normalise(v, st[0], st[1]);
 #pragma unroll
