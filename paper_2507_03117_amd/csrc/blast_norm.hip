@@ -81,13 +81,16 @@ int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
 // sixteen waves per CU of the full card.  From the sizes alone, so that the workspace does not depend on the device.
 constexpr int kBackwardRows = 512, kBackwardGroups = 256;
 
-template <int NW, int NCH, int TEAMS, bool VEC, bool LAYER, int MODE, int NL, bool LOW>
+template <int NW, int NCH, int TEAMS, bool VEC, bool AHEAD, bool LOW, bool LAYER, int MODE>
 int launch_backward_m(const NormArgs& a, hipStream_t stream) {
-  constexpr int kThreads = 64 * NW * TEAMS;
-  constexpr size_t kLds = (TEAMS > 1 ? (size_t)kThreads : (size_t)NL * 64 * NW) * NCH * 8 * 4;
+  constexpr int kThreads = 64 * NW * TEAMS, kSums = 1 + (MODE >= 1) + LAYER + (LAYER && MODE == 2);
+  constexpr size_t kSumBytes = (size_t)kThreads * NCH * 8 * 4;
+  // sums in LDS: as many as fit where a workgroup has a CU to itself, none where it has one row
+  constexpr int kFit = (int)((size_t)(150 << 10) / kSumBytes), NL = kThreads < 1024 ? 0 : kSums < kFit ? kSums : kFit;
+  constexpr size_t kLds = (size_t)NL * kSumBytes;
   const int64_t rows = (a.T + TEAMS - 1) / TEAMS;
-  const int64_t grid = TEAMS == 1 && a.T <= kBackwardRows ? a.T : rows < kBackwardGroups ? rows : kBackwardGroups;
-  constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, LOW>;
+  const int64_t grid = a.T <= kBackwardRows ? rows : rows < kBackwardGroups ? rows : kBackwardGroups;
+  constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, AHEAD, LOW>;
   if constexpr (kLds > 48 * 1024) {
     static blast::DeviceFlags lds_set;
     int dev = 0;
@@ -113,31 +116,38 @@ int launch_backward_m(const NormArgs& a, hipStream_t stream) {
   return BLAST_OK;
 }
 
-template <int NW, int NCH, int TEAMS, bool VEC, int NL = 0, bool LOW = false>
+template <int NW, int NCH, int TEAMS, bool VEC, bool AHEAD, bool LOW = false>
 int launch_backward(const NormArgs& a, hipStream_t stream) {
   const int mode = !a.y ? 0 : a.post ? 2 : 1;
   if (a.layer) {
-    if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, true, 0, NL, LOW>(a, stream);
-    if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, true, 1, NL, LOW>(a, stream);
-    return launch_backward_m<NW, NCH, TEAMS, VEC, true, 2, NL, LOW>(a, stream);
+    if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, true, 0>(a, stream);
+    if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, true, 1>(a, stream);
+    return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, true, 2>(a, stream);
   }
-  if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, false, 0, NL, LOW>(a, stream);
-  if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, false, 1, NL, LOW>(a, stream);
-  return launch_backward_m<NW, NCH, TEAMS, VEC, false, 2, NL, LOW>(a, stream);
+  if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, false, 0>(a, stream);
+  if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, false, 1>(a, stream);
+  return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, false, 2>(a, stream);
 }
 
 int dispatch_backward(const NormArgs& a, bool vec, hipStream_t stream) {
-  if (!vec) return a.width <= 2048 ? launch_backward<4, 1, 1, false>(a, stream) : launch_backward<16, 4, 1, false>(a, stream);
-  const bool few = a.T <= kBackwardRows;
+  if (!vec)
+    return a.width <= 2048 ? launch_backward<4, 1, 1, false, false>(a, stream) : launch_backward<16, 4, 1, false, false>(a, stream);
+  if (a.T <= kBackwardRows) {  // a row to a workgroup
+    if (a.width <= 512) return launch_backward<1, 1, 1, true, false>(a, stream);
+    if (a.width <= 1024) return launch_backward<2, 1, 1, true, false>(a, stream);
+    if (a.width <= 2048) return launch_backward<4, 1, 1, true, false>(a, stream);
+    if (a.width <= 4096) return launch_backward<8, 1, 1, true, false>(a, stream);
+  }
+  if (a.width <= 512) return launch_backward<1, 1, 16, true, true>(a, stream);
+  if (a.width <= 1024) return launch_backward<2, 1, 8, true, true>(a, stream);
+  if (a.width <= 2048) return launch_backward<4, 1, 4, true, true>(a, stream);
+  if (a.width <= 4096) return launch_backward<8, 1, 2, true, true>(a, stream);
+  if (a.width <= 8192) return launch_backward<16, 1, 1, true, true>(a, stream);
   const bool low = a.h_bf16 && a.dx_bf16 && (!a.w || a.p_bf16) &&
                    (!a.y || (a.y_bf16 && (!a.dy || a.dy_bf16) && (!a.gate || a.g_bf16) && ((!a.pw && !a.pb) || a.p_bf16)));
-  if (a.width <= 512) return few ? launch_backward<1, 1, 1, true>(a, stream) : launch_backward<1, 1, 16, true>(a, stream);
-  if (a.width <= 1024) return few ? launch_backward<2, 1, 1, true>(a, stream) : launch_backward<2, 1, 8, true>(a, stream);
-  if (a.width <= 2048) return few ? launch_backward<4, 1, 1, true>(a, stream) : launch_backward<4, 1, 4, true>(a, stream);
-  if (a.width <= 4096) return few ? launch_backward<8, 1, 1, true>(a, stream) : launch_backward<8, 1, 2, true>(a, stream);
-  if (a.width <= 8192) return launch_backward<16, 1, 1, true>(a, stream);
-  if (a.width <= 16384) return low ? launch_backward<16, 2, 1, true, 2, true>(a, stream) : launch_backward<16, 2, 1, true, 2>(a, stream);
-  return launch_backward<16, 4, 1, true>(a, stream);
+  if (a.width <= 16384)
+    return low ? launch_backward<16, 2, 1, true, true, true>(a, stream) : launch_backward<16, 2, 1, true, false>(a, stream);
+  return launch_backward<16, 4, 1, true, false>(a, stream);
 }
 
 }  // namespace
@@ -206,9 +216,9 @@ extern "C" int blast_norm_residual_backward(const blast_norm_view* P, const void
   NormArgs a = args_of(P, branch, T);
   const bool gate_sum = dgate && P->ldg == 0;
   a.sum_out[0] = dweight;
-  a.sum_out[1] = gate_sum ? static_cast<float*>(dgate) : nullptr;
-  a.sum_out[2] = dpost_weight;
-  a.sum_out[3] = dbias;
+  a.sum_out[1] = dbias;
+  a.sum_out[2] = gate_sum ? static_cast<float*>(dgate) : nullptr;
+  a.sum_out[3] = dpost_weight;
   a.sum_out[4] = dpost_bias;
   if (T == 0) {
     JoinArgs j{};

@@ -17,7 +17,7 @@ struct NormArgs {
   void *h_out, *x, *dh, *dy, *dgate;
   float* stats;
   float* part;  // column sums of the workgroups, [sum][workgroup][width]; with one workgroup the sums themselves
-  float* sum_out[5];  // slots: dweight, dgate, dpost_weight, dbias, dpost_bias (null: not wanted)
+  float* sum_out[5];  // dweight, dbias, dgate of one row, dpost_weight, dpost_bias (null: not wanted)
   int64_t ldh, ldy, ldg, ldho, ldx, lddx, lddh_in, lddh, lddy, lddg;
   int64_t T;
   int width;
@@ -140,56 +140,62 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
   }
 }
 
-// The gradient.  A workgroup holds TEAMS rows at a time, NW waves to a row, and goes over its share of the rows with the
-// columns' sums kept per lane: in registers, the first NL of them (dweight first) in LDS where a row leaves no registers for
-// them.  MODE: 0 no branch, 1 branch without a norm of its own, 2 with one.  LOW: every operand is bf16, whose pieces take half the
-// registers.
-template <int NW, int NCH, int TEAMS, bool VEC, bool LAYER, int MODE, int NL, bool LOW>
+// The gradient.  A workgroup holds TEAMS rows at a time, NW waves to a row, and goes over its share of the rows.  Over the
+// rows it keeps at most four sums per column, whatever is wanted of the branch:
+//     dx n (dweight),  dx (dbias),  q m,  q      with q = dh, times the gate where that has a row per token;
+// the gradients of a gate of one row, the branch's weight and its bias are those sums times factors of the column, applied at
+// the end.  The first NL of them are in LDS (a lane's own slots), the others in registers.
+// Rows one ahead (AHEAD): a tensor's registers take the next row's values as soon as this row's have been used, so that they
+// arrive during this row's sums and stores.  LOW: every operand is bf16, whose pieces take half the registers.
+// MODE: 0 no branch, 1 branch without a norm of its own, 2 with one.
+template <int NW, int NCH, int TEAMS, bool VEC, bool LAYER, int MODE, int NL, bool AHEAD, bool LOW>
 __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArgs a) {
-  static_assert(NL == 0 || TEAMS == 1, "sums in LDS are one row's");
   constexpr int NT = 64 * NW;
+  constexpr int kDw = 0, kQm = 1, kDx = 2, kQ = 3;
+  constexpr bool kSum[4] = {true, MODE >= 1, LAYER, LAYER && MODE == 2};
+  constexpr int kOrder[4] = {0, MODE >= 1 ? 1 : -1, !LAYER ? -1 : MODE >= 1 ? 2 : 1, LAYER && MODE == 2 ? 3 : -1};
+  constexpr auto in_lds = [](int s) { return kOrder[s] >= 0 && kOrder[s] < NL; };
+  static_assert(TEAMS == 1 || NL >= kOrder[0] + 1 + (MODE >= 1) + LAYER + (LAYER && MODE == 2), "the teams' sums meet in LDS");
   const int h_bf16 = LOW ? 1 : a.h_bf16, y_bf16 = LOW ? 1 : a.y_bf16, g_bf16 = LOW ? 1 : a.g_bf16, p_bf16 = LOW ? 1 : a.p_bf16;
   const int dx_bf16 = LOW ? 1 : a.dx_bf16, dy_bf16 = LOW ? 1 : a.dy_bf16;
-  // column sums: dweight | dgate | dpost_weight | dbias | dpost_bias, those that MODE and LAYER know
-  constexpr bool kSum[kNormSums] = {true, MODE >= 1, MODE == 2, LAYER, LAYER && MODE == 2};
-  constexpr int kInLds[kNormSums] = {NL > 0 ? 0 : -1, -1, NL > 1 ? 1 : -1, -1, -1};
   __shared__ float red[TEAMS][2][NW][2];
-  extern __shared__ __attribute__((aligned(16))) float pool[];  // sums in LDS [NL][NCH][2][NT][4], or where the teams' sums meet
-  const int team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT), lane = TEAMS == 1 ? threadIdx.x : threadIdx.x % NT;
+  extern __shared__ __attribute__((aligned(16))) float pool[];  // [sum][NCH][2][lane of the workgroup][4]
+  const int team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
+  const int lane = TEAMS == 1 ? threadIdx.x : threadIdx.x % NT;
   RowSum<NW> row_sum{red[team], lane >> 6};
   const int E = a.width;
   const float inv_e = 1.0f / (float)E;
-  float sum[kNormSums][NCH][8];
+  float sum[4][NCH][8];
+  auto slot = [&](int s, int c, int half, int of_team) {
+    return reinterpret_cast<float4*>(pool) + ((kOrder[s] * NCH + c) * 2 + half) * (NT * TEAMS) + of_team * NT + lane;
+  };
 #pragma unroll
-  for (int s = 0; s < kNormSums; ++s)
+  for (int s = 0; s < 4; ++s)
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
+    for (int c = 0; c < NCH; ++c) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[s][c][j] = 0.0f;
-  auto slot = [&](int s, int c, int half) { return reinterpret_cast<float4*>(pool) + ((kInLds[s] * NCH + c) * 2 + half) * NT + lane; };
-  if constexpr (NL > 0) {
-#pragma unroll
-    for (int s = 0; s < kNormSums; ++s)
-#pragma unroll
-      for (int c = 0; c < NCH; ++c)
-        if (kInLds[s] >= 0) *slot(s, c, 0) = *slot(s, c, 1) = float4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  // adds a piece's terms u v (or u alone) to sum s
-  auto accumulate = [&](auto s, int c, const float (&u)[8], const float (&v)[8]) {
-    if constexpr (kInLds[s.value] >= 0) {
+      if (in_lds(s)) *slot(s, c, 0, team) = *slot(s, c, 1, team) = float4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  // adds a piece's terms u v (without `v`: u) to a sum
+  auto accumulate = [&](auto which, int c, const float (&u)[8], const float (&v)[8]) {
+    constexpr int s = which.value;
+    constexpr bool plain = s == kDx || s == kQ;
+    if constexpr (in_lds(s)) {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        float4* q = slot(s.value, c, half);
+        float4* q = slot(s, c, half, team);
         float4 t = *q;
-        t.x = __builtin_fmaf(u[4 * half], v[4 * half], t.x);
-        t.y = __builtin_fmaf(u[4 * half + 1], v[4 * half + 1], t.y);
-        t.z = __builtin_fmaf(u[4 * half + 2], v[4 * half + 2], t.z);
-        t.w = __builtin_fmaf(u[4 * half + 3], v[4 * half + 3], t.w);
+        const int o = 4 * half;
+        t.x = plain ? t.x + u[o] : __builtin_fmaf(u[o], v[o], t.x);
+        t.y = plain ? t.y + u[o + 1] : __builtin_fmaf(u[o + 1], v[o + 1], t.y);
+        t.z = plain ? t.z + u[o + 2] : __builtin_fmaf(u[o + 2], v[o + 2], t.z);
+        t.w = plain ? t.w + u[o + 3] : __builtin_fmaf(u[o + 3], v[o + 3], t.w);
         *q = t;
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[s.value][c][j] = __builtin_fmaf(u[j], v[j], sum[s.value][c][j]);
+      for (int j = 0; j < 8; ++j) sum[s][c][j] = plain ? sum[s][c][j] + u[j] : __builtin_fmaf(u[j], v[j], sum[s][c][j]);
     }
   };
   auto inside = [&](int c, int j) { return piece_at<NT, VEC>(c, j, lane) < E; };
@@ -221,114 +227,135 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
       for (int j = 0; j < 8; ++j) v[j] *= f[j];
     }
   };
-  using S0 = std::integral_constant<int, 0>;
-  using S2 = std::integral_constant<int, 2>;
-  for (int64_t first = (int64_t)blockIdx.x * TEAMS; first < a.T; first += (int64_t)gridDim.x * TEAMS) {
-    // (a team without a row goes along on the last one, for the barriers, and keeps nothing)
-    const bool mine = TEAMS == 1 || first + team < a.T;
-    const int64_t t = mine ? first + team : a.T - 1;
+  auto plus = [&](float (&v)[8], const void* p, const Piece& q, int bf16) {
+    if (p) {
+      float f[8];
+      piece_values<VEC>(q, bf16, f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += f[j];
+    }
+  };
+  auto ask = [&](Piece& q, const void* p, int64_t at, int c, int bf16) {
+    if (p) piece_load<NT, VEC>(q, row_of(p, at, bf16), c, lane, E, bf16);
+  };
+  using Dw = std::integral_constant<int, kDw>;
+  using Qm = std::integral_constant<int, kQm>;
+  using Dx = std::integral_constant<int, kDx>;
+  using Q = std::integral_constant<int, kQ>;
+  const bool per_token = MODE >= 1 && a.gate && a.ldg != 0;
+  const int64_t step = (int64_t)gridDim.x * TEAMS;
+  // (a team without a row goes along on the last one, for the barriers, and keeps nothing)
+  auto row_at = [&](int64_t first) { return TEAMS == 1 || first + team < a.T ? first + team : a.T - 1; };
+  Piece h[NCH], dx[NCH], dhi[NCH], y[NCH], g[NCH];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) h[c] = dx[c] = dhi[c] = y[c] = g[c] = Piece{};
+  if constexpr (AHEAD) {
+    const int64_t t = row_at((int64_t)blockIdx.x * TEAMS);
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      ask(h[c], a.h, t * a.ldh, c, h_bf16);
+      ask(dx[c], a.dx, t * a.lddx, c, dx_bf16);
+      ask(dhi[c], a.dh_in, t * a.lddh_in, c, h_bf16);
+      if constexpr (MODE >= 1) {
+        ask(y[c], a.y, t * a.ldy, c, y_bf16);
+        ask(g[c], a.gate, t * a.ldg, c, g_bf16);
+      }
+    }
+  }
+  for (int64_t first = (int64_t)blockIdx.x * TEAMS; first < a.T; first += step) {
+    const bool mine = TEAMS == 1 || first + team < a.T, more = AHEAD && first + step < a.T;
+    const int64_t t = row_at(first), next = more ? row_at(first + step) : t;
     float d[NCH][8], n[NCH][8];
     const float4 st = scalar_float4(a.stats_in + t * 4);
-    Piece dhi[NCH], y[NCH], g[NCH], pw[NCH], pb[NCH];
+    Piece pw[NCH], pb[NCH];
     {
-      Piece h[NCH], dx[NCH], w[NCH];
+      Piece w[NCH];
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
-        h[c] = dx[c] = w[c] = Piece{};
-        piece_load<NT, VEC>(h[c], row_of(a.h, t * a.ldh, h_bf16), c, lane, E, h_bf16);
-        piece_load<NT, VEC>(dx[c], row_of(a.dx, t * a.lddx, dx_bf16), c, lane, E, dx_bf16);
-        if (a.w) piece_load<NT, VEC>(w[c], row_of(a.w, 0, p_bf16), c, lane, E, p_bf16);
+        if constexpr (!AHEAD) {
+          ask(h[c], a.h, t * a.ldh, c, h_bf16);
+          ask(dx[c], a.dx, t * a.lddx, c, dx_bf16);
+        }
+        w[c] = Piece{};
+        ask(w[c], a.w, 0, c, p_bf16);
       }
+      if constexpr (!AHEAD) {
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        dhi[c] = y[c] = Piece{};
-        if (a.dh_in) piece_load<NT, VEC>(dhi[c], row_of(a.dh_in, t * a.lddh_in, h_bf16), c, lane, E, h_bf16);
-        if constexpr (MODE >= 1) piece_load<NT, VEC>(y[c], row_of(a.y, t * a.ldy, y_bf16), c, lane, E, y_bf16);
+        for (int c = 0; c < NCH; ++c) {
+          ask(dhi[c], a.dh_in, t * a.lddh_in, c, h_bf16);
+          if constexpr (MODE >= 1) ask(y[c], a.y, t * a.ldy, c, y_bf16);
+        }
       }
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         piece_values<VEC>(h[c], h_bf16, n[c]);
         piece_values<VEC>(dx[c], dx_bf16, d[c]);
+        if (more) {
+          ask(h[c], a.h, next * a.ldh, c, h_bf16);
+          ask(dx[c], a.dx, next * a.lddx, c, dx_bf16);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) n[c][j] = inside(c, j) ? (n[c][j] - st.x) * st.y : 0.0f;
         if (mine) {
-          accumulate(S0{}, c, d[c], n[c]);
-          if constexpr (LAYER) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum[3][c][j] += d[c][j];
-          }
+          accumulate(Dw{}, c, d[c], n[c]);
+          if constexpr (LAYER) accumulate(Dx{}, c, d[c], d[c]);
         }
         times(d[c], a.w, w[c], p_bf16);
       }
     }
-    // (what the branch needs is asked for here: its registers were the stream's until now, and the row's sums take a while)
+    // (asked for while the row's sums are on their way)
     if constexpr (MODE >= 1) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
-        g[c] = Piece{};
-        if (a.gate) piece_load<NT, VEC>(g[c], row_of(a.gate, t * a.ldg, g_bf16), c, lane, E, g_bf16);
+        if constexpr (!AHEAD) ask(g[c], a.gate, t * a.ldg, c, g_bf16);
         if constexpr (MODE == 2) {
           pw[c] = pb[c] = Piece{};
-          if (a.pw) piece_load<NT, VEC>(pw[c], row_of(a.pw, 0, p_bf16), c, lane, E, p_bf16);
-          if (LAYER && a.pb) piece_load<NT, VEC>(pb[c], row_of(a.pb, 0, p_bf16), c, lane, E, p_bf16);
+          ask(pw[c], a.pw, 0, c, p_bf16);
+          if constexpr (LAYER)
+            if (per_token) ask(pb[c], a.pb, 0, c, p_bf16);
         }
       }
     }
     through(d, n, st.y);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-      if (a.dh_in) {
-        float f[8];
-        piece_values<VEC>(dhi[c], h_bf16, f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) d[c][j] += f[j];
-      }
+      plus(d[c], a.dh_in, dhi[c], h_bf16);
+      if (more) ask(dhi[c], a.dh_in, next * a.lddh_in, c, h_bf16);
       if (mine) piece_store<NT, VEC>(row_of(a.dh, t * a.lddh, h_bf16), c, lane, E, h_bf16, d[c]);
     }
     if constexpr (MODE >= 1) {
       // d: gradient of the stream.  n: y, or its normalised values
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
-        float p[8];
         piece_values<VEC>(y[c], y_bf16, n[c]);
+        if (more) ask(y[c], a.y, next * a.ldy, c, y_bf16);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (MODE == 2) n[c][j] = inside(c, j) ? (n[c][j] - st.z) * st.w : 0.0f;
-          p[j] = n[c][j];
           d[c][j] = inside(c, j) ? d[c][j] * a.scale : 0.0f;
         }
-        if (a.gate) {
-          if constexpr (MODE == 2) {
-            times(p, a.pw, pw[c], p_bf16);
-            if (LAYER && a.pb) {
-              float f[8];
-              piece_values<VEC>(pb[c], p_bf16, f);
+        if (per_token) {
+          if (a.dgate) {
+            float p[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) p[j] += f[j];
+            for (int j = 0; j < 8; ++j) p[j] = n[c][j];
+            if constexpr (MODE == 2) {
+              times(p, a.pw, pw[c], p_bf16);
+              if constexpr (LAYER) plus(p, a.pb, pb[c], p_bf16);
             }
-          }
 #pragma unroll
-          for (int j = 0; j < 8; ++j) p[j] *= d[c][j];
+            for (int j = 0; j < 8; ++j) p[j] *= d[c][j];
+            if (mine) piece_store<NT, VEC>(row_of(a.dgate, t * a.lddg, g_bf16), c, lane, E, g_bf16, p);
+          }
           times(d[c], a.gate, g[c], g_bf16);
-          if (mine) {
-            if (a.ldg == 0) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) sum[1][c][j] += p[j];
-            } else if (a.dgate) {
-              piece_store<NT, VEC>(row_of(a.dgate, t * a.lddg, g_bf16), c, lane, E, g_bf16, p);
-            }
-          }
         }
-        if constexpr (MODE == 2) {
-          if (mine) {
-            accumulate(S2{}, c, d[c], n[c]);
-            if constexpr (LAYER) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) sum[4][c][j] += d[c][j];
-            }
-          }
-          times(d[c], a.pw, pw[c], p_bf16);
+        if (mine) {
+          accumulate(Qm{}, c, d[c], n[c]);
+          if constexpr (kSum[kQ]) accumulate(Q{}, c, d[c], d[c]);
         }
+        if (!per_token) times(d[c], a.gate, g[c], g_bf16);
+        if (more) ask(g[c], a.gate, next * a.ldg, c, g_bf16);
+        if constexpr (MODE == 2) times(d[c], a.pw, pw[c], p_bf16);
       }
       if constexpr (MODE == 2) through(d, n, st.w);
       if (a.dy && mine) {
@@ -337,42 +364,74 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
       }
     }
   }
-  // ---- the workgroup's column sums
-  float* out = a.part;
+  // ---- the workgroup's column sums, of its teams in order, and what they are the gradients of
+  if constexpr (TEAMS > 1) {
+    __syncthreads();
+    if (team != 0) return;
+  }
 #pragma unroll
-  for (int s = 0; s < kNormSums; ++s) {
-    if (!kSum[s] || !a.sum_out[s]) continue;
-    float* dst = gridDim.x == 1 ? a.sum_out[s] : out + (int64_t)blockIdx.x * E;
-    out += (int64_t)gridDim.x * E;
-    if constexpr (TEAMS > 1) {
-      __syncthreads();
+  for (int c = 0; c < NCH; ++c) {
 #pragma unroll
-      for (int c = 0; c < NCH; ++c)
+    for (int s = 0; s < 4; ++s) {
+      if (!in_lds(s)) continue;
+#pragma unroll 1
+      for (int k = 0; k < TEAMS; ++k)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) pool[team * (NT * NCH * 8) + piece_at<NT, VEC>(c, j, lane)] = sum[s][c][j];
-      __syncthreads();
-      for (int e = threadIdx.x; e < E; e += NT * TEAMS) {
-        float v = pool[e];
+        for (int half = 0; half < 2; ++half) {
+          const float4 v = *slot(s, c, half, k);
+          const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int k = 1; k < TEAMS; ++k) v += pool[k * (NT * NCH * 8) + e];
-        dst[e] = v;
+          for (int j = 0; j < 4; ++j) sum[s][c][4 * half + j] = k == 0 ? f[j] : sum[s][c][4 * half + j] + f[j];
+        }
+    }
+    float* part = a.part;
+    auto put = [&](float* to, const float (&v)[8]) {
+      if (!to) return;
+      if (gridDim.x == 1) {  // (a caller's array may lie anywhere)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (inside(c, j)) to[piece_at<NT, VEC>(c, j, lane)] = v[j];
+        return;
       }
-    } else {
+      piece_store<NT, VEC>(row_of(part, (int64_t)blockIdx.x * E, 0), c, lane, E, 0, v);
+      part += (int64_t)gridDim.x * E;
+    };
+    put(a.sum_out[0], sum[kDw][c]);
+    if constexpr (LAYER) put(a.sum_out[1], sum[kDx][c]);
+    if constexpr (MODE >= 1) {
+      Piece qg{}, qw{}, qb{};
+      const bool one_row = a.gate && !per_token;
+      if (one_row) ask(qg, a.gate, 0, c, g_bf16);
+      if constexpr (MODE == 2) {
+        ask(qw, a.pw, 0, c, p_bf16);
+        if constexpr (LAYER) ask(qb, a.pb, 0, c, p_bf16);
+      }
+      float v[8];
+      if (a.sum_out[2]) {  // gate of one row: post_weight sum(q m) + post_bias sum(q)
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        if constexpr (NL > 0) {
-          if (kInLds[s] >= 0) {
-            const float4 lo = *slot(s, c, 0), hi = *slot(s, c, 1);
-            const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        for (int j = 0; j < 8; ++j) v[j] = sum[kQm][c][j];
+        if constexpr (MODE == 2) times(v, a.pw, qw, p_bf16);
+        if constexpr (kSum[kQ]) {
+          float b[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[s][c][j] = v[j];
+          for (int j = 0; j < 8; ++j) b[j] = sum[kQ][c][j];
+          if (a.pb) {
+            times(b, a.pb, qb, p_bf16);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += b[j];
           }
         }
+        put(a.sum_out[2], v);
+      }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int e = piece_at<NT, VEC>(c, j, lane);
-          if (e < E) dst[e] = sum[s][c][j];
-        }
+      for (int j = 0; j < 8; ++j) v[j] = sum[kQm][c][j];
+      if (one_row) times(v, a.gate, qg, g_bf16);
+      put(a.sum_out[3], v);
+      if constexpr (kSum[kQ]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = sum[kQ][c][j];
+        if (one_row) times(v, a.gate, qg, g_bf16);
+        put(a.sum_out[4], v);
       }
     }
   }
