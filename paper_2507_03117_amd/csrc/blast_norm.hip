@@ -81,13 +81,14 @@ int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
 // sixteen waves per CU of the full card.  From the sizes alone, so that the workspace does not depend on the device.
 constexpr int kBackwardRows = 512, kBackwardGroups = 256;
 
-template <int NW, int NCH, int TEAMS, bool VEC, bool AHEAD, bool LOW, bool LAYER, int MODE>
+template <int NW, int NCH, int TEAMS, bool VEC, bool ROOM, bool LOW, bool LAYER, int MODE>
 int launch_backward_m(const NormArgs& a, hipStream_t stream) {
   constexpr int kThreads = 64 * NW * TEAMS, kSums = 1 + (MODE >= 1) + LAYER + (LAYER && MODE == 2);
   constexpr size_t kSumBytes = (size_t)kThreads * NCH * 8 * 4;
   // sums in LDS: as many as fit where a workgroup has a CU to itself, none where it has one row
   constexpr int kFit = (int)((size_t)(150 << 10) / kSumBytes), NL = kThreads < 1024 ? 0 : kSums < kFit ? kSums : kFit;
   constexpr size_t kLds = (size_t)NL * kSumBytes;
+  constexpr bool AHEAD = ROOM && !(NCH > 1 && LAYER && MODE >= 1);  // (two sums of a layer norm are then in registers)
   const int64_t rows = (a.T + TEAMS - 1) / TEAMS;
   const int64_t grid = a.T <= kBackwardRows ? rows : rows < kBackwardGroups ? rows : kBackwardGroups;
   constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, AHEAD, LOW>;

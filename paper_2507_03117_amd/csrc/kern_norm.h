@@ -236,6 +236,7 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
     }
   };
   auto ask = [&](Piece& q, const void* p, int64_t at, int c, int bf16) {
+    if (!AHEAD) q = Piece{};  // (or what a row left in it would stay in registers until the next)
     if (p) piece_load<NT, VEC>(q, row_of(p, at, bf16), c, lane, E, bf16);
   };
   using Dw = std::integral_constant<int, kDw>;
@@ -243,6 +244,7 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
   using Dx = std::integral_constant<int, kDx>;
   using Q = std::integral_constant<int, kQ>;
   const bool per_token = MODE >= 1 && a.gate && a.ldg != 0;
+  const bool want_qm = a.sum_out[2] || a.sum_out[3], want_q = (a.sum_out[2] && a.pb) || a.sum_out[4];
   const int64_t step = (int64_t)gridDim.x * TEAMS;
   // (a team without a row goes along on the last one, for the barriers, and keeps nothing)
   auto row_at = [&](int64_t first) { return TEAMS == 1 || first + team < a.T ? first + team : a.T - 1; };
@@ -279,12 +281,9 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
         w[c] = Piece{};
         ask(w[c], a.w, 0, c, p_bf16);
       }
-      if constexpr (!AHEAD) {
-#pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-          ask(dhi[c], a.dh_in, t * a.lddh_in, c, h_bf16);
-          if constexpr (MODE >= 1) ask(y[c], a.y, t * a.ldy, c, y_bf16);
-        }
+      if constexpr (!AHEAD && NCH == 1) {
+        ask(dhi[0], a.dh_in, t * a.lddh_in, 0, h_bf16);
+        if constexpr (MODE >= 1) ask(y[0], a.y, t * a.ldy, 0, y_bf16);
       }
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
@@ -297,14 +296,15 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
 #pragma unroll
         for (int j = 0; j < 8; ++j) n[c][j] = inside(c, j) ? (n[c][j] - st.x) * st.y : 0.0f;
         if (mine) {
-          accumulate(Dw{}, c, d[c], n[c]);
-          if constexpr (LAYER) accumulate(Dx{}, c, d[c], d[c]);
+          if (a.sum_out[0]) accumulate(Dw{}, c, d[c], n[c]);
+          if constexpr (LAYER)
+            if (a.sum_out[1]) accumulate(Dx{}, c, d[c], d[c]);
         }
         times(d[c], a.w, w[c], p_bf16);
       }
     }
-    // (asked for while the row's sums are on their way)
-    if constexpr (MODE >= 1) {
+    // Asked for while the row's sums are on their way.  Wide rows in turn: what the branch reads after the stream is stored.
+    auto ask_branch = [&]() {
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         if constexpr (!AHEAD) ask(g[c], a.gate, t * a.ldg, c, g_bf16);
@@ -315,6 +315,14 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
             if (per_token) ask(pb[c], a.pb, 0, c, p_bf16);
         }
       }
+    };
+    constexpr bool kInTurn = !AHEAD && NCH > 1;
+    if constexpr (kInTurn) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) ask(dhi[c], a.dh_in, t * a.lddh_in, c, h_bf16);
+    } else if constexpr (MODE >= 1) {
+      ask_branch();
     }
     through(d, n, st.y);
 #pragma unroll
@@ -324,6 +332,12 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
       if (mine) piece_store<NT, VEC>(row_of(a.dh, t * a.lddh, h_bf16), c, lane, E, h_bf16, d[c]);
     }
     if constexpr (MODE >= 1) {
+      if constexpr (kInTurn) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) ask(y[c], a.y, t * a.ldy, c, y_bf16);
+        ask_branch();
+      }
       // d: gradient of the stream.  n: y, or its normalised values
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
@@ -350,8 +364,9 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
           times(d[c], a.gate, g[c], g_bf16);
         }
         if (mine) {
-          accumulate(Qm{}, c, d[c], n[c]);
-          if constexpr (kSum[kQ]) accumulate(Q{}, c, d[c], d[c]);
+          if (want_qm) accumulate(Qm{}, c, d[c], n[c]);
+          if constexpr (kSum[kQ])
+            if (want_q) accumulate(Q{}, c, d[c], d[c]);
         }
         if (!per_token) times(d[c], a.gate, g[c], g_bf16);
         if (more) ask(g[c], a.gate, next * a.ldg, c, g_bf16);
