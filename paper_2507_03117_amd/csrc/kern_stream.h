@@ -474,7 +474,11 @@ __device__ __forceinline__ void stream_epilogue(const Epilogue& e, f32x16 (&acc)
         if (whole.value || dt < lane_left) {
           if constexpr (C::PAIR) {
             typedef __bf16 Bf16Pair __attribute__((ext_vector_type(2)));
-            *reinterpret_cast<Bf16Pair*>(p) = Bf16Pair{static_cast<__bf16>(acc[mi][0][j]), static_cast<__bf16>(acc[mi][1][j])};
+            const Bf16Pair z{static_cast<__bf16>(acc[mi][0][j]), static_cast<__bf16>(acc[mi][1][j])};
+            if constexpr (B == 128)  // (see the stores of Y)
+              __builtin_nontemporal_store(z, reinterpret_cast<Bf16Pair*>(p));
+            else
+              store_through(reinterpret_cast<Bf16Pair*>(p), z);
           } else {
 #pragma unroll
             for (int ni = 0; ni < C::NI; ++ni) *reinterpret_cast<uint16_t*>(p + ni * kStep * 2) = f32_to_bf16_rne(acc[mi][ni][j]);
@@ -992,11 +996,15 @@ __global__ __launch_bounds__(64 * NW, (StreamCfg<B, TW, NW, F8>::WAVES_PER_SIMD)
     //   128-wide blocks in E5M2: non-temporal, or through where the launch says so (y_keep, see there).  The output is the
     //     larger part of what moves, and the last-level cache keeps the inputs instead of it: 53248 x 16384, 1000 tokens, with
     //     the quantiser 95 / 93 / 78, cold 111 / 109 / 114; 2048 tokens, fp32 output 180 / 182 / 157, cold 183 / 183 / 171.
+    //   128-wide blocks with an epilogue of their own: non-temporal, Z too.  Rows of few blocks write more than they read, and the
+    //     L2 keeps the activations instead: 14336 x 4096 at 95 %, 4096 tokens, ordinary / non-temporal 57.6 / 44.2, with SiLU 63.6 /
+    //     50.5, with Z 75.7 / 61.5; with the 4096 x 14336 product that reads it behind it 101.8 / 103.0, with Z 124.4 / 111.1; 4096
+    //     and 14336 at 80 %, 2048 tokens, both products 133.6 / 131.2; 16384 and 53248 at 95 %, 1024 tokens 271.4 / 271.4.
     //   An output whose rows may not be stored in pairs: ordinary, so that the L2 puts lines together that are written in
     //     parts.  (Through or past it with rows two apart: up to 1.9 times as long; 8192 x 3072 at 70 %, 64-wide, 2048 tokens,
     //     odd pitch, fp32 47.0 / 61.5 us, in E5M2 with 14336 x 4096 at 90 %, 128-wide, bf16 29.3 / 56.0.)
     enum { kStoreOrdinary, kStoreThrough, kStoreStreaming };
-    constexpr int kStores = B < 128 ? kStoreThrough : F8 ? kStoreStreaming : kStoreOrdinary;
+    constexpr int kStores = B < 128 ? kStoreThrough : F8 || EPI::kOn ? kStoreStreaming : kStoreOrdinary;
     if (a.y_fast && !(CHUNK && shared_row)) {
       const uint32_t esz = a.y_bf16 ? 2u : 4u;
       unsigned char* base = reinterpret_cast<unsigned char*>(a.Y) + (int64_t)t0 * a.syt * esz;
