@@ -57,23 +57,33 @@ bool params_pieces_ok(const NormArgs& a) {
          blast::aligned(a.pb, 16) && pieces_ok(a.gate, a.ldg, a.g_bf16 ? BLAST_BF16 : BLAST_F32);
 }
 
-template <int NW, int NCH, bool VEC>
+// A row (with one wave to a row, four) to a workgroup while several workgroups fit on a CU: the others' loads cover one's
+// sums (16 waves a CU that go over the rows, one ahead / a row each, microseconds: 4096 x 4096, branch with a norm 29.8 / 26.0; 2048
+// x 8192 33.3 / 31.1; one row of 4096 3.5 / 3.0).  Rows of more than 8192 take a CU for themselves: a workgroup per CU goes over them, one
+// ahead (2048 x 16384, gate per token 80.1 / 66.0; layer norms 85.9 / 67.3).
+template <int NW, int NCH, bool VEC, bool AHEAD = false, bool LOW = false>
 int launch_forward(const NormArgs& a, hipStream_t stream) {
   constexpr int kRows = NW == 1 ? 4 : 1;
-  const int64_t grid = (a.T + kRows - 1) / kRows;
-  k_norm_residual<NW, NCH, VEC><<<dim3((unsigned)grid), dim3(NW == 1 ? 256 : 64 * NW), 0, stream>>>(a);
+  int64_t grid = (a.T + kRows - 1) / kRows;
+  constexpr bool kLoop = NW * NCH > 16;
+  if (kLoop && grid > 256) grid = 256;
+  k_norm_residual<NW, NCH, VEC, kLoop, AHEAD, LOW><<<dim3((unsigned)grid), dim3(NW == 1 ? 256 : 64 * NW), 0, stream>>>(a);
   BLAST_LAUNCH_CHECK("k_norm_residual");
   return BLAST_OK;
 }
 
 int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
-  if (!vec) return a.width <= 2048 ? launch_forward<4, 1, false>(a, stream) : launch_forward<16, 4, false>(a, stream);
+  if (!vec) {
+    if (a.width <= 2048) return launch_forward<4, 1, false>(a, stream);
+    return a.width <= 8192 ? launch_forward<16, 1, false>(a, stream) : launch_forward<16, 4, false>(a, stream);
+  }
   if (a.width <= 512) return launch_forward<1, 1, true>(a, stream);
   if (a.width <= 1024) return launch_forward<2, 1, true>(a, stream);
   if (a.width <= 2048) return launch_forward<4, 1, true>(a, stream);
   if (a.width <= 4096) return launch_forward<8, 1, true>(a, stream);
   if (a.width <= 8192) return launch_forward<16, 1, true>(a, stream);
-  if (a.width <= 16384) return launch_forward<16, 2, true>(a, stream);
+  const bool low = a.h_bf16 && (!a.w || a.p_bf16) && (!a.y || (a.y_bf16 && (!a.gate || a.g_bf16) && ((!a.pw && !a.pb) || a.p_bf16)));
+  if (a.width <= 16384) return low ? launch_forward<16, 2, true, true, true>(a, stream) : launch_forward<16, 2, true>(a, stream);
   return launch_forward<16, 4, true>(a, stream);
 }
 
@@ -131,8 +141,10 @@ int launch_backward(const NormArgs& a, hipStream_t stream) {
 }
 
 int dispatch_backward(const NormArgs& a, bool vec, hipStream_t stream) {
-  if (!vec)
-    return a.width <= 2048 ? launch_backward<4, 1, 1, false, false>(a, stream) : launch_backward<16, 4, 1, false, false>(a, stream);
+  if (!vec) {
+    if (a.width <= 2048) return launch_backward<4, 1, 1, false, false>(a, stream);
+    return a.width <= 8192 ? launch_backward<16, 1, 1, false, false>(a, stream) : launch_backward<16, 4, 1, false, false>(a, stream);
+  }
   if (a.T <= kBackwardRows) {  // a row to a workgroup
     if (a.width <= 512) return launch_backward<1, 1, 1, true, false>(a, stream);
     if (a.width <= 1024) return launch_backward<2, 1, 1, true, false>(a, stream);

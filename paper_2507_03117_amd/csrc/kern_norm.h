@@ -28,21 +28,21 @@ struct NormArgs {
 
 constexpr int kNormSums = 5;
 
-template <int NW, int NCH, bool VEC>
+// LOOP: a workgroup goes over its share of the rows, else it has one.  AHEAD, LOW: see the gradient.
+template <int NW, int NCH, bool VEC, bool LOOP, bool AHEAD, bool LOW>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const NormArgs a) {
   constexpr int NT = 64 * NW, ROWS = NW == 1 ? 4 : 1;
+  const int h_bf16 = LOW ? 1 : a.h_bf16, y_bf16 = LOW ? 1 : a.y_bf16, g_bf16 = LOW ? 1 : a.g_bf16, p_bf16 = LOW ? 1 : a.p_bf16;
   __shared__ float red[2][NW][2];
   const int lane = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
-  const int64_t t = (int64_t)blockIdx.x * ROWS + (NW == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
-  if (t >= a.T) return;  // (whole waves; with NW > 1 whole workgroups)
   RowSum<NW> row_sum{red, (int)(threadIdx.x >> 6)};
   const int E = a.width;
   const float inv_e = 1.0f / (float)E;
   const bool branch = a.y != nullptr;
-  auto ask = [&](Piece (&q)[NCH], const void* p, int64_t at, int bf16) {
+  auto ask = [&](Piece (&q)[NCH], const void* p, int64_t at, int bf16, bool fresh) {
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-      q[c] = Piece{};
+      if (fresh) q[c] = Piece{};
       if (p) piece_load<NT, VEC>(q[c], row_of(p, at, bf16), c, lane, E, bf16);
     }
   };
@@ -78,65 +78,78 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
   auto affine = [&](float (&v)[8], const Piece& weight, bool has_weight, const Piece& bias, bool has_bias) {
     float f[8];
     if (has_weight) {
-      piece_values<VEC>(weight, a.p_bf16, f);
+      piece_values<VEC>(weight, p_bf16, f);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= f[j];
     }
     if (has_bias) {
-      piece_values<VEC>(bias, a.p_bf16, f);
+      piece_values<VEC>(bias, p_bf16, f);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += f[j];
     }
   };
-  float v[NCH][8], st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  Piece h[NCH], g[NCH], w[NCH], b[NCH];
-  if (branch) {
-    Piece y[NCH], pw[NCH], pb[NCH];
-    float p[NCH][8];
-    ask(y, a.y, t * a.ldy, a.y_bf16);
-    ask(h, a.h, t * a.ldh, a.h_bf16);
-    ask(g, a.gate, t * a.ldg, a.g_bf16);
-    ask(pw, a.pw, 0, a.p_bf16);
-    ask(pb, a.pb, 0, a.p_bf16);
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  int64_t t = (int64_t)blockIdx.x * ROWS + (NW == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+  Piece h[NCH], y[NCH], g[NCH];
+  auto ask_row = [&](int64_t row, bool fresh) {
+    ask(y, a.y, row * a.ldy, y_bf16, fresh);
+    ask(h, a.h, row * a.ldh, h_bf16, fresh);
+    ask(g, a.gate, row * a.ldg, g_bf16, fresh);
+  };
+  if (t >= a.T) return;  // (with NW > 1 the whole workgroup has the row)
+  if (AHEAD) ask_row(t, true);
+  auto row = [&]() {
+    const bool more = AHEAD && t + step < a.T;
+    if (!AHEAD) ask_row(t, true);
+    float v[NCH][8], st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    Piece w[NCH], b[NCH];
+    if (branch) {
+      Piece pw[NCH], pb[NCH];
+      float p[NCH][8];
+      ask(pw, a.pw, 0, p_bf16, true);
+      ask(pb, a.pb, 0, p_bf16, true);
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) piece_values<VEC>(y[c], a.y_bf16, p[c]);
-    if (a.post) {
-      normalise(p, st[2], st[3]);
+      for (int c = 0; c < NCH; ++c) piece_values<VEC>(y[c], y_bf16, p[c]);
+      if (more) ask(y, a.y, (t + step) * a.ldy, y_bf16, false);
+      if (a.post) {
+        normalise(p, st[2], st[3]);
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) affine(p[c], pw[c], a.pw != nullptr, pb[c], a.pb != nullptr);
-    }
-#pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      piece_values<VEC>(h[c], a.h_bf16, v[c]);
-      if (a.gate) {
-        float f[8];
-        piece_values<VEC>(g[c], a.g_bf16, f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) p[c][j] *= f[j];
+        for (int c = 0; c < NCH; ++c) affine(p[c], pw[c], a.pw != nullptr, pb[c], a.pb != nullptr);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[c][j] = __builtin_fmaf(a.scale, p[c][j], v[c][j]);
-      piece_store<NT, VEC>(row_of(a.h_out, t * a.ldho, a.h_bf16), c, lane, E, a.h_bf16, v[c]);
+      for (int c = 0; c < NCH; ++c) {
+        piece_values<VEC>(h[c], h_bf16, v[c]);
+        if (a.gate) {
+          float f[8];
+          piece_values<VEC>(g[c], g_bf16, f);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[c][j] *= f[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[c][j] = __builtin_fmaf(a.scale, p[c][j], v[c][j]);
+        piece_store<NT, VEC>(row_of(a.h_out, t * a.ldho, h_bf16), c, lane, E, h_bf16, v[c]);
+      }
+      if (more) ask(g, a.gate, (t + step) * a.ldg, g_bf16, false);
+    } else {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) piece_values<VEC>(h[c], h_bf16, v[c]);
     }
+    if (more) ask(h, a.h, (t + step) * a.ldh, h_bf16, false);
+    // (in registers that the branch no longer needs; the row's sums take a while)
+    ask(w, a.w, 0, p_bf16, true);
+    ask(b, a.b, 0, p_bf16, true);
+    normalise(v, st[0], st[1]);
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      affine(v[c], w[c], a.w != nullptr, b[c], a.b != nullptr);
+      piece_store<NT, VEC>(row_of(a.x, t * a.ldx, a.x_bf16), c, lane, E, a.x_bf16, v[c]);
+    }
+    if (a.stats && lane == 0) *reinterpret_cast<float4*>(a.stats + t * 4) = float4{st[0], st[1], st[2], st[3]};
+  };
+  if constexpr (LOOP) {
+    for (; t < a.T; t += step) row();
   } else {
-    ask(h, a.h, t * a.ldh, a.h_bf16);
-  }
-  // (in registers that the branch no longer needs; the row's sums take a while)
-  ask(w, a.w, 0, a.p_bf16);
-  ask(b, a.b, 0, a.p_bf16);
-  if (!branch) {
-#pragma unroll
-    for (int c = 0; c < NCH; ++c) piece_values<VEC>(h[c], a.h_bf16, v[c]);
-  }
-  normalise(v, st[0], st[1]);
-#pragma unroll
-  for (int c = 0; c < NCH; ++c) {
-    affine(v[c], w[c], a.w != nullptr, b[c], a.b != nullptr);
-    piece_store<NT, VEC>(row_of(a.x, t * a.ldx, a.x_bf16), c, lane, E, a.x_bf16, v[c]);
-  }
-  if (a.stats && lane == 0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a.stats[t * 4 + i] = st[i];
+    row();
   }
 }
 
