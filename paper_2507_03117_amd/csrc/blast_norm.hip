@@ -65,9 +65,12 @@ template <int NW, int NCH, bool VEC, bool AHEAD = false, bool LOW = false>
 int launch_forward(const NormArgs& a, hipStream_t stream) {
   constexpr int kRows = NW == 1 ? 4 : 1;
   int64_t grid = (a.T + kRows - 1) / kRows;
-  constexpr bool kLoop = NW * NCH > 16;
-  if (kLoop && grid > 256) grid = 256;
-  k_norm_residual<NW, NCH, VEC, kLoop, AHEAD, LOW><<<dim3((unsigned)grid), dim3(NW == 1 ? 256 : 64 * NW), 0, stream>>>(a);
+  constexpr int kThreads = NW == 1 ? 256 : 64 * NW;
+  if (NW * NCH > 16 && grid > 256) {
+    k_norm_residual<NW, NCH, VEC, (NW * NCH > 16), AHEAD, LOW><<<dim3(256), dim3(kThreads), 0, stream>>>(a);
+  } else {
+    k_norm_residual<NW, NCH, VEC, false, false, LOW><<<dim3((unsigned)grid), dim3(kThreads), 0, stream>>>(a);
+  }
   BLAST_LAUNCH_CHECK("k_norm_residual");
   return BLAST_OK;
 }
