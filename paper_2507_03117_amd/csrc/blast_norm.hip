@@ -94,17 +94,17 @@ int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
 // sixteen waves per CU of the full card.  From the sizes alone, so that the workspace does not depend on the device.
 constexpr int kBackwardRows = 512, kBackwardGroups = 256;
 
-template <int NW, int NCH, int TEAMS, bool VEC, bool ROOM, bool LOW, bool LAYER, int MODE>
+template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW, bool LAYER, int MODE>
 int launch_backward_m(const NormArgs& a, hipStream_t stream) {
   constexpr int kThreads = 64 * NW * TEAMS, kSums = 1 + (MODE >= 1) + LAYER + (LAYER && MODE == 2);
   constexpr size_t kSumBytes = (size_t)kThreads * NCH * 8 * 4;
-  // sums in LDS: as many as fit where a workgroup has a CU to itself, none where it has one row
-  constexpr int kFit = (int)((size_t)(150 << 10) / kSumBytes), NL = kThreads < 1024 ? 0 : kSums < kFit ? kSums : kFit;
+  // sums in LDS: as many as fit, the workgroup having a CU to itself; none where it has one row
+  constexpr int kFit = (int)((size_t)(150 << 10) / kSumBytes), NL = !LOOP ? 0 : kSums < kFit ? kSums : kFit;
   constexpr size_t kLds = (size_t)NL * kSumBytes;
-  constexpr bool AHEAD = ROOM && !(NCH > 1 && LAYER && MODE >= 1);  // (two sums of a layer norm are then in registers)
+  constexpr bool AHEAD = LOOP && ROOM && !(NCH > 1 && LAYER && MODE >= 1);  // (two sums of a layer norm are then in registers)
   const int64_t rows = (a.T + TEAMS - 1) / TEAMS;
-  const int64_t grid = a.T <= kBackwardRows ? rows : rows < kBackwardGroups ? rows : kBackwardGroups;
-  constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, AHEAD, LOW>;
+  const int64_t grid = LOOP && rows > kBackwardGroups ? kBackwardGroups : rows;
+  constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, LOOP, AHEAD, LOW>;
   if constexpr (kLds > 48 * 1024) {
     static blast::DeviceFlags lds_set;
     int dev = 0;
@@ -130,40 +130,43 @@ int launch_backward_m(const NormArgs& a, hipStream_t stream) {
   return BLAST_OK;
 }
 
-template <int NW, int NCH, int TEAMS, bool VEC, bool AHEAD, bool LOW = false>
+template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW = false>
 int launch_backward(const NormArgs& a, hipStream_t stream) {
   const int mode = !a.y ? 0 : a.post ? 2 : 1;
   if (a.layer) {
-    if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, true, 0>(a, stream);
-    if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, true, 1>(a, stream);
-    return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, true, 2>(a, stream);
+    if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, true, 0>(a, stream);
+    if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, true, 1>(a, stream);
+    return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, true, 2>(a, stream);
   }
-  if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, false, 0>(a, stream);
-  if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, false, 1>(a, stream);
-  return launch_backward_m<NW, NCH, TEAMS, VEC, AHEAD, LOW, false, 2>(a, stream);
+  if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, 0>(a, stream);
+  if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, 1>(a, stream);
+  return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, 2>(a, stream);
 }
 
 int dispatch_backward(const NormArgs& a, bool vec, hipStream_t stream) {
   if (!vec) {
-    if (a.width <= 2048) return launch_backward<4, 1, 1, false, false>(a, stream);
-    return a.width <= 8192 ? launch_backward<16, 1, 1, false, false>(a, stream) : launch_backward<16, 4, 1, false, false>(a, stream);
+    if (a.width <= 2048) return launch_backward<4, 1, 1, false, true, false>(a, stream);
+    return a.width <= 8192 ? launch_backward<16, 1, 1, false, true, false>(a, stream) : launch_backward<16, 4, 1, false, true, false>(a, stream);
   }
-  if (a.T <= kBackwardRows) {  // a row to a workgroup
-    if (a.width <= 512) return launch_backward<1, 1, 1, true, false>(a, stream);
-    if (a.width <= 1024) return launch_backward<2, 1, 1, true, false>(a, stream);
-    if (a.width <= 2048) return launch_backward<4, 1, 1, true, false>(a, stream);
-    if (a.width <= 4096) return launch_backward<8, 1, 1, true, false>(a, stream);
-  }
-  if (a.width <= 512) return launch_backward<1, 1, 16, true, true>(a, stream);
-  if (a.width <= 1024) return launch_backward<2, 1, 8, true, true>(a, stream);
-  if (a.width <= 2048) return launch_backward<4, 1, 4, true, true>(a, stream);
-  if (a.width <= 4096) return launch_backward<8, 1, 2, true, true>(a, stream);
-  if (a.width <= 8192) return launch_backward<16, 1, 1, true, true>(a, stream);
   const bool low = a.h_bf16 && a.dx_bf16 && (!a.w || a.p_bf16) &&
                    (!a.y || (a.y_bf16 && (!a.dy || a.dy_bf16) && (!a.gate || a.g_bf16) && ((!a.pw && !a.pb) || a.p_bf16)));
+  if (a.T <= kBackwardRows) {  // a row to a workgroup
+    if (a.width <= 512) return launch_backward<1, 1, 1, true, false, false>(a, stream);
+    if (a.width <= 1024) return launch_backward<2, 1, 1, true, false, false>(a, stream);
+    if (a.width <= 2048) return launch_backward<4, 1, 1, true, false, false>(a, stream);
+    if (a.width <= 4096) return launch_backward<8, 1, 1, true, false, false>(a, stream);
+    if (a.width <= 8192) return launch_backward<16, 1, 1, true, false, false>(a, stream);
+    if (a.width <= 16384)
+      return low ? launch_backward<16, 2, 1, true, false, false, true>(a, stream) : launch_backward<16, 2, 1, true, false, false>(a, stream);
+  }
+  if (a.width <= 512) return launch_backward<1, 1, 16, true, true, true>(a, stream);
+  if (a.width <= 1024) return launch_backward<2, 1, 8, true, true, true>(a, stream);
+  if (a.width <= 2048) return launch_backward<4, 1, 4, true, true, true>(a, stream);
+  if (a.width <= 4096) return launch_backward<8, 1, 2, true, true, true>(a, stream);
+  if (a.width <= 8192) return launch_backward<16, 1, 1, true, true, true>(a, stream);
   if (a.width <= 16384)
-    return low ? launch_backward<16, 2, 1, true, true, true>(a, stream) : launch_backward<16, 2, 1, true, false>(a, stream);
-  return launch_backward<16, 4, 1, true, false>(a, stream);
+    return low ? launch_backward<16, 2, 1, true, true, true, true>(a, stream) : launch_backward<16, 2, 1, true, true, false>(a, stream);
+  return launch_backward<16, 4, 1, true, true, false>(a, stream);
 }
 
 }  // namespace

@@ -160,8 +160,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
 // the end.  The first NL of them are in LDS (a lane's own slots), the others in registers.
 // Rows one ahead (AHEAD): a tensor's registers take the next row's values as soon as this row's have been used, so that they
 // arrive during this row's sums and stores.  LOW: every operand is bf16, whose pieces take half the registers.
-// MODE: 0 no branch, 1 branch without a norm of its own, 2 with one.
-template <int NW, int NCH, int TEAMS, bool VEC, bool LAYER, int MODE, int NL, bool AHEAD, bool LOW>
+// LOOP = false: a workgroup has its TEAMS rows and no others.  MODE: 0 no branch, 1 branch without a norm of its own, 2 with one.
+template <int NW, int NCH, int TEAMS, bool VEC, bool LAYER, int MODE, int NL, bool LOOP, bool AHEAD, bool LOW>
 __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArgs a) {
   constexpr int NT = 64 * NW;
   constexpr int kDw = 0, kQm = 1, kDx = 2, kQ = 3;
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
       }
     }
   }
-  for (int64_t first = (int64_t)blockIdx.x * TEAMS; first < a.T; first += step) {
+  auto rows = [&](int64_t first) {
     const bool mine = TEAMS == 1 || first + team < a.T, more = AHEAD && first + step < a.T;
     const int64_t t = row_at(first), next = more ? row_at(first + step) : t;
     float d[NCH][8], n[NCH][8];
@@ -391,6 +391,11 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
         for (int c = 0; c < NCH; ++c) piece_store<NT, VEC>(row_of(a.dy, t * a.lddy, dy_bf16), c, lane, E, dy_bf16, d[c]);
       }
     }
+  };
+  if constexpr (LOOP) {
+    for (int64_t first = (int64_t)blockIdx.x * TEAMS; first < a.T; first += step) rows(first);
+  } else {
+    rows((int64_t)blockIdx.x * TEAMS);
   }
   // ---- the workgroup's column sums, of its teams in order, and what they are the gradients of
   if constexpr (TEAMS > 1) {
