@@ -188,6 +188,43 @@ def test_linear_layouts_pitches_and_places(b, T):
                      what="in place", at={"residual": stream, "out": stream})
 
 
+@pytest.mark.parametrize("b,rows,cols,T", [(128, 8192, 512, 1030), (128, 1024, 512, 700), (64, 8192, 512, 1030), (64, 2048, 512, 1030), (32, 2048, 512, 515),
+                                           (16, 512, 512, 515)])
+@pytest.mark.parametrize("odd", ["none", "y", "r", "z", "all"])
+def test_linear_large_tiles_with_odd_pitches(b, rows, cols, T, odd):
+    """The kernels of many tokens store and read two rows at a time where every operand allows it, and only there; a last tile
+    that the tokens end in; the residual in place."""
+    packed, dense = matrix(rows + b, rows, cols, b, 0.3)
+    d = dense.to(DEV)
+    x, bias = rand(T, (T, cols), torch.bfloat16).to(DEV), rand(5, (rows,)).to(DEV)
+    z64 = torch.matmul(x.double(), d.t().contiguous()) + bias.double()
+    slack = (cols + 2) * U * (torch.matmul(x.double().abs(), d.abs().t().contiguous()) + bias.double().abs())
+    for r_type, y_type in ((torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)):
+        r = rand(6, (T, rows), r_type)
+        place = lambda t, n: wide(t, 3, 1) if odd in (n, "all") else t.to(DEV)  # noqa: E731
+        rd, y, z = place(r, "r"), place(torch.zeros(T, rows, dtype=y_type), "y"), place(torch.zeros(T, rows, dtype=torch.bfloat16), "z")
+        api.bsr_linear(packed, x, bias=bias, act="relu", residual=rd, pre=z, out=y)
+        close(z, z64, slack, "z")
+        y64 = z64.clamp_min(0) + r.to(DEV).double()
+        close(y, y64, slack + U * (r.to(DEV).double().abs() + y64.abs()), "y")
+        same = place(r, "r")
+        api.bsr_linear(packed, x, bias=bias, residual=same, out=same)
+        y64 = z64 + r.to(DEV).double()
+        close(same, y64, slack + U * (r.to(DEV).double().abs() + y64.abs()), "in place")
+
+
+@pytest.mark.parametrize("b", [32, 64, 128])
+def test_linear_activations_beyond_32_bit_offsets(b):
+    """More tokens than 32-bit offsets into X reach: token ranges of their own, whose residual, Z and Y move along."""
+    packed, dense = matrix(b, 256, 256, b, 0.7)
+    T, pitch = 600, 4 << 20
+    buf = torch.empty((T - 1) * pitch + 256, dtype=torch.bfloat16, device=DEV)
+    x = torch.as_strided(buf, (T, 256), (pitch, 1))
+    host = rand(1, (T, 256), torch.bfloat16)
+    x.copy_(host)
+    check_linear(packed, dense, host, rand(2, (256,)), "silu", rand(3, (T, 256)), "bf16", True, what="long", at={"x": x})
+
+
 def test_linear_without_blocks_tokens_or_epilogue():
     """No stored block: act(bias) + residual.  No token: nothing.  No epilogue: the bits of bsr_spmm in bf16."""
     for b in (16, 64, 128):
@@ -214,6 +251,23 @@ def test_linear_offsets_beyond_32_bits():
     places[0].copy_(r)
     check_linear(packed, dense, x, None, "silu", r, "bf16", True, what="far",
                  at={"residual": places[0], "pre": places[1], "out": places[2]})
+
+
+def test_row_operators_beyond_32_bit_offsets():
+    """Rows more than 2^31 elements apart in one buffer."""
+    pitch = (1 << 30) + 8
+    buf = torch.empty(3 * pitch, dtype=torch.bfloat16, device=DEV)
+    place = lambda at, t: torch.as_strided(buf, t.shape, (pitch, 1), at).copy_(t)  # noqa: E731
+    z, u, dy = (rand(k, (3, 72), torch.bfloat16) for k in range(3))
+    far = [place(128 * k, t) for k, t in enumerate((z, u, dy))]
+    api._act_backward(*far, "silu", far[0], far[1], far[2], None, None)
+    check_act(z, u, dy, "silu", False, {"dz": far[0], "du": far[1], "h": far[2]}, "far")
+    s = norm_inputs(5, 3, 72, "layer", "bf16", "bf16", "f32", True, "tokens")
+    s["args"]["gate"] = s["args"]["gate"].bfloat16()
+    at = {"h": place(1024, s["h"]), "y": place(1152, s["y"]), "h_out": place(1280, s["h"]), "out": place(1408, s["h"])}
+    check_forward(s, "far", **at)
+    at = {"h": place(1024, s["h"]), "y": place(1152, s["y"]), "dx": place(1280, s["dx"]), "dh": place(1408, s["dh"]), "to": place(1536, s["h"])}
+    check_backward(s, "far", **at)
 
 
 # ---- gradient of an activation -----------------------------------------------------------------------------------------------
