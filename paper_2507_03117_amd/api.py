@@ -705,7 +705,7 @@ def _act_backward(Z, U, dY, act, dZ, dU, H, dbias_z, dbias_u):
         wsb = C.c_size_t(0)
         _check(L.blast_act_backward_workspace(T, N, wanted, C.byref(wsb)), "blast_act_backward_workspace")
         ws_bytes = wsb.value
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dY.device) if ws_bytes else None
+        ws = dY.new_empty(ws_bytes, dtype=torch.uint8) if ws_bytes else None
     _check(L.blast_act_backward(*_rows_of(Z, shape, low), *_rows_of(U, shape, low), *_rows_of(dY, shape, _EITHER),
                                 _dtype_code(dY.dtype), T, N, ACT_NONE if act is None else ACT[act], *_rows_of(dZ, shape, low),
                                 *_rows_of(dU, shape, low), *_rows_of(H, shape, low), _ptr(dbias_z), _ptr(dbias_u), _ptr(ws),
@@ -717,7 +717,7 @@ def act_backward(Z: Optional[torch.Tensor], dY: torch.Tensor, *, act: Optional[s
     """blast_act_backward of one matrix: dZ = dY * act'(Z) (bf16) and, with bias_grad, dbias = its sum over the tokens.
     Z: the `pre` of bsr_linear, bf16 [T, N]; None without an activation."""
     dZ = out if out is not None else torch.empty_like(dY, dtype=torch.bfloat16)
-    db = torch.empty(dY.shape[1], dtype=torch.float32, device=dY.device) if bias_grad else None
+    db = dY.new_empty(dY.shape[1], dtype=torch.float32) if bias_grad else None
     _act_backward(Z, None, dY, act, dZ, None, None, db, None)
     return ActGrads(dZ=dZ, dbias=db)
 
@@ -731,7 +731,7 @@ def gated_act_backward(G: torch.Tensor, U: torch.Tensor, dH: torch.Tensor, *, ac
     H = torch.empty_like(dH, dtype=torch.bfloat16) if with_h else None
     dbg = dbu = None
     if bias_grad:
-        dbg, dbu = (torch.empty(dH.shape[1], dtype=torch.float32, device=dH.device) for _ in range(2))
+        dbg, dbu = dH.new_empty(dH.shape[1], dtype=torch.float32), dH.new_empty(dH.shape[1], dtype=torch.float32)
     _act_backward(G, U, dH, act, dG, dU, H, dbg, dbu)
     return ActGrads(None, None, dG, dU, H, dbg, dbu)
 
@@ -780,7 +780,7 @@ def norm_residual(h: torch.Tensor, y: Optional[torch.Tensor] = None, *, kind: st
     T, E = h.shape
     new_h = h if y is None else h_out if h_out is not None else torch.empty_like(h)
     x = out if out is not None else torch.empty_like(h, dtype=out_dtype)
-    stats = torch.empty((T, 4), dtype=torch.float32, device=h.device) if with_stats else None
+    stats = h.new_empty((T, 4), dtype=torch.float32) if with_stats else None
     v = _norm_view(E, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
     _check(lib().blast_norm_residual(v, *_norm_args(h, y, new_h, x, stats), _stream()), "blast_norm_residual")
     return (new_h, x, stats) if with_stats else (new_h, x)
@@ -823,11 +823,9 @@ def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats
     L = lib()
     assert h_out.dim() == 2
     T, E = h_out.shape
-    dev = h_out.device
     shape, h_dtype = h_out.shape, h_out.dtype
     v = _norm_view(E, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
     branch, same = y is not None, (h_dtype,)
-    sums = {"dtype": torch.float32, "device": dev}
     dh = dh if dh is not None else torch.empty_like(h_out)
     dy = dgate = dpost_weight = dpost_bias = None
     dyp, lddy, lddg = None, 0, 0
@@ -836,15 +834,15 @@ def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats
         dyp, lddy = _rows_of(dy, shape, _EITHER)
         if gate is not None:
             if gate.dim() == 1:
-                dgate = torch.empty(E, **sums)
+                dgate = torch.empty_like(gate, dtype=torch.float32)
             else:
                 dgate = torch.empty_like(gate)
                 lddg = _rows_of(dgate, shape, _EITHER)[1]
         if post:
-            dpost_weight = None if post_weight is None else torch.empty(E, **sums)
-            dpost_bias = None if post_bias is None else torch.empty(E, **sums)
-    dweight = None if weight is None else torch.empty(E, **sums)
-    dbias = None if bias is None else torch.empty(E, **sums)
+            dpost_weight = None if post_weight is None else torch.empty_like(post_weight, dtype=torch.float32)
+            dpost_bias = None if post_bias is None else torch.empty_like(post_bias, dtype=torch.float32)
+    dweight = None if weight is None else torch.empty_like(weight, dtype=torch.float32)
+    dbias = None if bias is None else torch.empty_like(bias, dtype=torch.float32)
     assert stats.is_cuda and stats.dtype == torch.float32 and stats.shape == (T, 4) and stats.is_contiguous()
     hp, ldh = _rows_of(h_out, shape, _EITHER)
     yp, ldy = _rows_of(y, shape, _EITHER)
@@ -855,7 +853,7 @@ def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats
     _check(L.blast_norm_residual_backward_workspace(v, T, C.byref(wsb)), "blast_norm_residual_backward_workspace")
     ws_bytes = wsb.value
     if ws_bytes:
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+        ws = dx.new_empty(ws_bytes, dtype=torch.uint8)
     _check(L.blast_norm_residual_backward(
         v, hp, ldh, _dtype_code(h_dtype), yp, ldy, _dtype_code(y.dtype) if branch else F32, stats.data_ptr(), dxp, lddx,
         _dtype_code(dx.dtype), dhop, lddho, T, dhp, lddh, dyp, lddy, _dtype_code(dy_dtype), _ptr(dgate), lddg, _ptr(dweight),
