@@ -94,8 +94,14 @@ int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
 // sixteen waves per CU of the full card.  From the sizes alone, so that the workspace does not depend on the device.
 constexpr int kBackwardRows = 512, kBackwardGroups = 256;
 
-template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW, bool LAYER, int MODE>
-int launch_backward_m(const NormArgs& a, hipStream_t stream) {
+// Few rows: the columns have workgroups of their own in the launch of the rows, instead of a second launch that joins the rows'
+// sums, where no other sums are wanted than those of the norm of the stream.
+bool columns_owned(int64_t T, bool branch, int post, bool gate_of_one_row) {
+  return T <= kBackwardRows && (!branch || (!post && !gate_of_one_row));
+}
+
+template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW, bool COLS, bool LAYER, int MODE>
+int launch_backward_m(NormArgs a, hipStream_t stream) {
   constexpr int kThreads = 64 * NW * TEAMS, kSums = 1 + (MODE >= 1) + LAYER + (LAYER && MODE == 2);
   constexpr size_t kSumBytes = (size_t)kThreads * NCH * 8 * 4;
   // sums in LDS: as many as fit, the workgroup having a CU to itself; none where it has one row
@@ -103,8 +109,12 @@ int launch_backward_m(const NormArgs& a, hipStream_t stream) {
   constexpr size_t kLds = (size_t)NL * kSumBytes;
   constexpr bool AHEAD = LOOP && ROOM && !(NCH > 1 && LAYER && MODE >= 1);  // (two sums of a layer norm are then in registers)
   const int64_t rows = (a.T + TEAMS - 1) / TEAMS;
-  const int64_t grid = LOOP && rows > kBackwardGroups ? kBackwardGroups : rows;
-  constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, LOOP, AHEAD, LOW>;
+  int64_t grid = LOOP && rows > kBackwardGroups ? kBackwardGroups : rows;
+  if constexpr (COLS) {
+    if (a.sum_out[0] || a.sum_out[1]) a.column_groups = (a.width + 16 * kNormOwned - 1) / (16 * kNormOwned) * 16;
+    grid += a.column_groups;
+  }
+  constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, LOOP, AHEAD, LOW, COLS>;
   if constexpr (kLds > 48 * 1024) {
     static blast::DeviceFlags lds_set;
     int dev = 0;
@@ -116,7 +126,7 @@ int launch_backward_m(const NormArgs& a, hipStream_t stream) {
   }
   kernel<<<dim3((unsigned)grid), dim3(kThreads), kLds, stream>>>(a);
   BLAST_LAUNCH_CHECK("k_norm_backward");
-  if (grid == 1) return BLAST_OK;
+  if (COLS || grid == 1) return BLAST_OK;
   JoinArgs j{};
   j.part = a.part;
   j.groups = (int)grid;
@@ -130,27 +140,37 @@ int launch_backward_m(const NormArgs& a, hipStream_t stream) {
   return BLAST_OK;
 }
 
+template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW, bool LAYER>
+int launch_backward_k(const NormArgs& a, hipStream_t stream) {
+  const int mode = !a.y ? 0 : a.post ? 2 : 1;
+  if constexpr (!LOOP) {
+    if (columns_owned(a.T, a.y != nullptr, a.post, a.gate && a.ldg == 0)) {
+      if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, false, false, LOW, true, LAYER, 0>(a, stream);
+      return launch_backward_m<NW, NCH, TEAMS, VEC, false, false, LOW, true, LAYER, 1>(a, stream);
+    }
+  } else {
+    if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, true, ROOM, LOW, false, LAYER, 0>(a, stream);
+  }
+  if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, LAYER, 1>(a, stream);
+  return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, LAYER, 2>(a, stream);
+}
+
 template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW = false>
 int launch_backward(const NormArgs& a, hipStream_t stream) {
-  const int mode = !a.y ? 0 : a.post ? 2 : 1;
-  if (a.layer) {
-    if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, true, 0>(a, stream);
-    if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, true, 1>(a, stream);
-    return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, true, 2>(a, stream);
-  }
-  if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, 0>(a, stream);
-  if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, 1>(a, stream);
-  return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, 2>(a, stream);
+  return a.layer ? launch_backward_k<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, true>(a, stream)
+                 : launch_backward_k<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false>(a, stream);
 }
 
 int dispatch_backward(const NormArgs& a, bool vec, hipStream_t stream) {
+  const bool few = a.T <= kBackwardRows;  // a row to a workgroup
   if (!vec) {
-    if (a.width <= 2048) return launch_backward<4, 1, 1, false, true, false>(a, stream);
-    return a.width <= 8192 ? launch_backward<16, 1, 1, false, true, false>(a, stream) : launch_backward<16, 4, 1, false, true, false>(a, stream);
+    if (a.width <= 2048) return few ? launch_backward<4, 1, 1, false, false, false>(a, stream) : launch_backward<4, 1, 1, false, true, false>(a, stream);
+    if (a.width <= 8192) return few ? launch_backward<16, 1, 1, false, false, false>(a, stream) : launch_backward<16, 1, 1, false, true, false>(a, stream);
+    return few ? launch_backward<16, 4, 1, false, false, false>(a, stream) : launch_backward<16, 4, 1, false, true, false>(a, stream);
   }
   const bool low = a.h_bf16 && a.dx_bf16 && (!a.w || a.p_bf16) &&
                    (!a.y || (a.y_bf16 && (!a.dy || a.dy_bf16) && (!a.gate || a.g_bf16) && ((!a.pw && !a.pb) || a.p_bf16)));
-  if (a.T <= kBackwardRows) {  // a row to a workgroup
+  if (few) {
     if (a.width <= 512) return launch_backward<1, 1, 1, true, false, false>(a, stream);
     if (a.width <= 1024) return launch_backward<2, 1, 1, true, false, false>(a, stream);
     if (a.width <= 2048) return launch_backward<4, 1, 1, true, false, false>(a, stream);
@@ -158,6 +178,7 @@ int dispatch_backward(const NormArgs& a, bool vec, hipStream_t stream) {
     if (a.width <= 8192) return launch_backward<16, 1, 1, true, false, false>(a, stream);
     if (a.width <= 16384)
       return low ? launch_backward<16, 2, 1, true, false, false, true>(a, stream) : launch_backward<16, 2, 1, true, false, false>(a, stream);
+    return launch_backward<16, 4, 1, true, false, false>(a, stream);
   }
   if (a.width <= 512) return launch_backward<1, 1, 16, true, true, true>(a, stream);
   if (a.width <= 1024) return launch_backward<2, 1, 8, true, true, true>(a, stream);
@@ -209,7 +230,8 @@ extern "C" int blast_norm_residual_backward_workspace(const blast_norm_view* P, 
   if (T < 0 || T > INT32_MAX / 2 || !ws_bytes) return BLAST_ERR_INVALID_ARG;
   const int layer = P->kind == BLAST_NORM_LAYER;
   const int sums = 1 + layer + (P->post ? 1 + layer : 0) + (P->gate && P->ldg == 0 ? 1 : 0);
-  *ws_bytes = T <= 1 ? 0 : (size_t)sums * (size_t)(T < kBackwardRows ? T : kBackwardRows) * (size_t)P->width * 4;
+  // (without a branch fewer sums are wanted: the size serves that call as well)
+  *ws_bytes = T <= 1 || columns_owned(T, true, P->post, P->gate && P->ldg == 0) ? 0 : (size_t)sums * (size_t)(T < kBackwardRows ? T : kBackwardRows) * (size_t)P->width * 4;
   return BLAST_OK;
 }
 
@@ -256,6 +278,7 @@ extern "C" int blast_norm_residual_backward(const blast_norm_view* P, const void
   if (!stats || !blast::aligned(stats, 16)) return BLAST_ERR_INVALID_ARG;
   size_t need = 0;
   if (int rc = blast_norm_residual_backward_workspace(P, T, &need)) return rc;
+  if (!branch && columns_owned(T, false, 0, false)) need = 0;
   if (need > 0 && (!ws || ws_bytes < need || !blast::aligned(ws, 16))) return BLAST_ERR_WORKSPACE;
   a.part = static_cast<float*>(ws);
   a.h = h_out;

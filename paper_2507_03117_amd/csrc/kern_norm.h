@@ -24,6 +24,7 @@ struct NormArgs {
   int h_bf16, y_bf16, g_bf16, p_bf16, x_bf16, dx_bf16, dy_bf16;
   int layer, post;
   float eps, scale;
+  int column_groups;  // workgroups of a gradient launch that own columns (see norm_columns)
 };
 
 constexpr int kNormSums = 5;
@@ -153,6 +154,72 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
   }
 }
 
+// dweight and dbias of 32 columns over all rows: they need the statistics but no sum over a row, so that workgroups beside
+// those of the rows can have them, in the same launch, where there are few rows.  Four lanes to a row, two rows of a lane on
+// their way at a time; two neighbouring workgroups of an XCD (ids eight apart) share the 128-byte lines of bf16.
+constexpr int kNormOwned = 32;
+template <int THREADS, bool VEC, bool LAYER>
+__device__ __forceinline__ void norm_columns(const NormArgs& a, int id) {
+  constexpr int kLanes = kNormOwned / 8, kRows = THREADS / kLanes, kWaves = THREADS / 64;
+  __shared__ float red[kWaves][kNormOwned];
+  const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
+  const int col0 = ((id / 16) * 16 + (id % 8) * 2 + id / 8 % 2) * kNormOwned;
+  const int width = a.width - col0 < kNormOwned ? a.width - col0 : kNormOwned;
+  if (width <= 0) return;
+  float sum[2][8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[0][j] = sum[1][j] = 0.0f;
+  struct Row {
+    Piece h, dx;
+    float2 st;
+  };
+  auto read = [&](Row& q, int t) {
+    q.h = q.dx = Piece{};
+    piece_load<kLanes, VEC>(q.h, row_of(a.h, t * a.ldh + col0, a.h_bf16), 0, lane, width, a.h_bf16);
+    piece_load<kLanes, VEC>(q.dx, row_of(a.dx, t * a.lddx + col0, a.dx_bf16), 0, lane, width, a.dx_bf16);
+    q.st = *reinterpret_cast<const float2*>(a.stats_in + (int64_t)t * 4);
+  };
+  auto add = [&](const Row& q) {
+    float n[8], d[8];
+    piece_values<VEC>(q.h, a.h_bf16, n);
+    piece_values<VEC>(q.dx, a.dx_bf16, d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      sum[0][j] = __builtin_fmaf(d[j], (n[j] - q.st.x) * q.st.y, sum[0][j]);
+      if (LAYER) sum[1][j] += d[j];
+    }
+  };
+  for (int t = team; t < a.T; t += 2 * kRows) {
+    Row q0, q1;
+    read(q0, t);
+    const bool two = t + kRows < a.T;
+    if (two) read(q1, t + kRows);
+    add(q0);
+    if (two) add(q1);
+  }
+  // the sixteen rows of a wave, then the waves in order
+#pragma unroll
+  for (int s = 0; s < (LAYER ? 2 : 1); ++s) {
+    if (!a.sum_out[s]) continue;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float v = sum[s][j];
+#pragma unroll
+      for (int m = kLanes; m < 64; m *= 2) v += __shfl_xor(v, m);
+      if ((threadIdx.x & 63) < kLanes) red[threadIdx.x >> 6][piece_at<kLanes, VEC>(0, j, lane)] = v;
+    }
+    __syncthreads();
+    const int e = threadIdx.x;
+    if (e < width) {
+      float v = red[0][e];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) v += red[w][e];
+      a.sum_out[s][col0 + e] = v;
+    }
+  }
+}
+
 // The gradient.  A workgroup holds TEAMS rows at a time, NW waves to a row, and goes over its share of the rows.  Over the
 // rows it keeps at most four sums per column, whatever is wanted of the branch:
 //     dx n (dweight),  dx (dbias),  q m,  q      with q = dh, times the gate where that has a row per token;
@@ -160,12 +227,20 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
 // the end.  The first NL of them are in LDS (a lane's own slots), the others in registers.
 // Rows one ahead (AHEAD): a tensor's registers take the next row's values as soon as this row's have been used, so that they
 // arrive during this row's sums and stores.  LOW: every operand is bf16, whose pieces take half the registers.
-// LOOP = false: a workgroup has its TEAMS rows and no others.  MODE: 0 no branch, 1 branch without a norm of its own, 2 with one.
-template <int NW, int NCH, int TEAMS, bool VEC, bool LAYER, int MODE, int NL, bool LOOP, bool AHEAD, bool LOW>
+// LOOP = false: a workgroup has its TEAMS rows and no others.  COLS: the first workgroups own columns instead, and the others keep
+// no sums.  MODE: 0 no branch, 1 branch without a norm of its own, 2 with one.
+template <int NW, int NCH, int TEAMS, bool VEC, bool LAYER, int MODE, int NL, bool LOOP, bool AHEAD, bool LOW, bool COLS>
 __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArgs a) {
   constexpr int NT = 64 * NW;
+  static_assert(!COLS || (!LOOP && TEAMS == 1 && MODE < 2), "few rows, and sums that need no other over a row");
+  if constexpr (COLS) {
+    if ((int)blockIdx.x < a.column_groups) {
+      norm_columns<NT, VEC, LAYER>(a, blockIdx.x);
+      return;
+    }
+  }
   constexpr int kDw = 0, kQm = 1, kDx = 2, kQ = 3;
-  constexpr bool kSum[4] = {true, MODE >= 1, LAYER, LAYER && MODE == 2};
+  constexpr bool kSum[4] = {true, MODE >= 1, LAYER, LAYER && MODE == 2};  // those that MODE and LAYER know
   constexpr int kOrder[4] = {0, MODE >= 1 ? 1 : -1, !LAYER ? -1 : MODE >= 1 ? 2 : 1, LAYER && MODE == 2 ? 3 : -1};
   constexpr auto in_lds = [](int s) { return kOrder[s] >= 0 && kOrder[s] < NL; };
   static_assert(TEAMS == 1 || NL >= kOrder[0] + 1 + (MODE >= 1) + LAYER + (LAYER && MODE == 2), "the teams' sums meet in LDS");
@@ -308,7 +383,7 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) n[c][j] = inside(c, j) ? (n[c][j] - st.x) * st.y : 0.0f;
-        if (mine) {
+        if (mine && !COLS) {
           if (a.sum_out[0]) accumulate(Dw{}, c, d[c], n[c]);
           if constexpr (LAYER)
             if (a.sum_out[1]) accumulate(Dx{}, c, d[c], d[c]);
@@ -376,7 +451,7 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
           }
           times(d[c], a.gate, g[c], g_bf16);
         }
-        if (mine) {
+        if (mine && !COLS) {
           if (want_qm) accumulate(Qm{}, c, d[c], n[c]);
           if constexpr (kSum[kQ])
             if (want_q) accumulate(Q{}, c, d[c], d[c]);
@@ -395,7 +470,8 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
   if constexpr (LOOP) {
     for (int64_t first = (int64_t)blockIdx.x * TEAMS; first < a.T; first += step) rows(first);
   } else {
-    rows((int64_t)blockIdx.x * TEAMS);
+    rows((int64_t)(COLS ? blockIdx.x - a.column_groups : blockIdx.x) * TEAMS);
+    if constexpr (COLS) return;
   }
   // ---- the workgroup's column sums, of its teams in order, and what they are the gradients of
   if constexpr (TEAMS > 1) {

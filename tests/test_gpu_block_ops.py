@@ -312,6 +312,16 @@ def test_act_backward_sizes(T, N, act, gated):
         check_act(z, u, dy, act, bias_grad, run_act(z, u, dy, act, bias_grad, with_h=k != 1), f"{T}x{N} {dtype}")
 
 
+@pytest.mark.parametrize("T", [63, 64, 65, 255, 256, 257, 511, 512, 513, 1024])
+@pytest.mark.parametrize("N", [8, 31, 32, 40, 512, 520, 1000])
+def test_act_backward_sums_at_the_seams(T, N):
+    """Row counts at which the columns' sums change hands, widths that end inside a workgroup's columns."""
+    z, u = rand(T, (T, N), torch.bfloat16, 2.0).to(DEV), rand(N, (T, N), torch.bfloat16).to(DEV)
+    dy = rand(T + N, (T, N)).to(DEV)
+    for gate in (None, u):
+        check_act(z, gate, dy, "silu", True, run_act(z, gate, dy, "silu", True), f"{T}x{N}")
+
+
 def test_act_backward_over_the_range_of_bf16():
     """Every finite bf16 value of the pre-activation: slopes at zeros of both signs, in the tails and beyond them."""
     bits = torch.arange(65536, dtype=torch.int32).to(torch.int16)
@@ -582,6 +592,16 @@ def test_norm_backward_pitches_and_places(E):
     g = api.norm_residual_backward(s["h"].to(DEV), None, torch.cat([torch.zeros(21, 1), torch.ones(21, 3)], 1).to(DEV), s["dx"].to(DEV), d, dh=d)
     want = api.norm_residual_backward(s["h"].to(DEV), None, torch.cat([torch.zeros(21, 1), torch.ones(21, 3)], 1).to(DEV), s["dx"].to(DEV), s["dh"].to(DEV))
     assert g.dh is d and torch.equal(d, want.dh)
+
+
+@pytest.mark.parametrize("T", [1, 2, 31, 32, 33, 511, 512, 513, 1030])
+@pytest.mark.parametrize("E", [8, 24, 40, 129, 520, 1600])
+def test_norm_backward_sums_at_the_seams(T, E):
+    """Row counts at which the columns' sums change hands, widths that end inside a workgroup's columns, with and without the
+    branch's own sums."""
+    for kind, y, post, gate in (("layer", None, False, None), ("rms", "bf16", False, "tokens"), ("layer", "bf16", False, "vector"),
+                                ("layer", "f32", True, "tokens"), ("rms", "bf16", True, "vector")):
+        check_backward(norm_inputs(T + E, T, E, kind, "f32", y, "f32", post, gate), f"{T}x{E} {kind} {post} {gate}")
 
 
 def test_norm_backward_over_no_rows_and_repeatability():
