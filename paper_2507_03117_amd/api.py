@@ -627,7 +627,7 @@ def _rows_of(t: Optional[torch.Tensor], shape, dtypes):
 def _vector(t: Optional[torch.Tensor], n: int, dtypes):
     if t is None:
         return None
-    assert t.is_cuda and t.shape == (n,) and t.dtype in dtypes and (n <= 1 or t.stride(0) == 1)
+    assert t.is_cuda and t.dim() == 1 and t.numel() == n and t.dtype in dtypes and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -826,18 +826,21 @@ def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats
     shape, h_dtype = h_out.shape, h_out.dtype
     v = _norm_view(E, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
     branch, same = y is not None, (h_dtype,)
-    dh = dh if dh is not None else torch.empty_like(h_out)
+    if dh is None:
+        dh = torch.empty_like(h_out)  # (what is made here is contiguous)
+        dhp, lddh = dh.data_ptr(), E
+    else:
+        dhp, lddh = _rows_of(dh, shape, same)
     dy = dgate = dpost_weight = dpost_bias = None
     dyp, lddy, lddg = None, 0, 0
     if branch:
         dy = torch.empty_like(h_out, dtype=dy_dtype)
-        dyp, lddy = _rows_of(dy, shape, _EITHER)
+        dyp, lddy = dy.data_ptr(), E
         if gate is not None:
             if gate.dim() == 1:
                 dgate = torch.empty_like(gate, dtype=torch.float32)
             else:
-                dgate = torch.empty_like(gate)
-                lddg = _rows_of(dgate, shape, _EITHER)[1]
+                dgate, lddg = torch.empty_like(gate), E
         if post:
             dpost_weight = None if post_weight is None else torch.empty_like(post_weight, dtype=torch.float32)
             dpost_bias = None if post_bias is None else torch.empty_like(post_bias, dtype=torch.float32)
@@ -848,7 +851,6 @@ def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats
     yp, ldy = _rows_of(y, shape, _EITHER)
     dxp, lddx = _rows_of(dx, shape, _EITHER)
     dhop, lddho = _rows_of(dh_out, shape, same)
-    dhp, lddh = _rows_of(dh, shape, same)
     wsb, ws = C.c_size_t(0), None
     _check(L.blast_norm_residual_backward_workspace(v, T, C.byref(wsb)), "blast_norm_residual_backward_workspace")
     ws_bytes = wsb.value
