@@ -10,7 +10,9 @@
  * (Sec. 3.2, Sec. 3.4.1), the mask update of the prune-and-grow step with its sparsity
  * schedule (Sec. 3.2: Listing 1 and Eq. (2)), the pooled top-k mask used for
  * post-training sparsification (Sec. 3.3) and the product on 8-bit E5M2
- * operands (Sec. 5.2).
+ * operands (Sec. 5.2); and what a transformer block and its training step put next
+ * to those products: bias, activation and residual in a product's epilogue, the
+ * gradient through an activation, the norms with the residual add.
  *
  * Conventions
  *  - Weights are `out x in`, row-major, like a linear layer's weight: W is
@@ -504,7 +506,7 @@ int blast_bsr_gated_spmm(const blast_bsr_view* Wgate, const blast_bsr_view* Wup,
  *   act                      BLAST_ACT_NONE, _SILU, _GELU or _RELU
  *   R, ldr, r_dtype          residual in the layout of X, fp32 or bf16, may be NULL; may be Y itself (same pitch and type)
  *   Y, ldy, y_dtype          out, in the layout of X, fp32 or bf16
- *   Z, ldz                   out, bf16 in the layout of X, may be NULL: what blast_act_backward reads; must not overlap Y
+ *   Z, ldz                   out, bf16 in the layout of X, may be NULL: what blast_act_backward reads; overlaps neither Y nor R
  *   ws, ws_bytes             as in blast_bsr_spmm: blast_bsr_spmm_workspace() bytes, optional
  * Never synchronises.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED_BLOCK, HIP.
  */
@@ -582,7 +584,7 @@ int blast_norm_residual(const blast_norm_view* P, const void* h, int64_t ldh, in
  *   h_out, y, stats     what the forward call wrote and read (y NULL as there)
  *   dx, lddx, dx_dtype  gradient of x, fp32 or bf16
  *   dh_out, lddho       gradient of h_out through the rest of the stream, h_dtype, may be NULL (zero)
- *   dh, lddh            out, h_dtype; may be dh_out (same pitch)
+ *   dh, lddh            out, h_dtype; may be dh_out (same pitch); no other output overlaps an input
  *   dy, lddy, dy_dtype  out, fp32 or bf16, may be NULL
  *   dgate, lddg         out, may be NULL: with P->ldg = 0 fp32 [width], the sum over the tokens; else [T][width] in g_dtype
  *   dweight, dbias, dpost_weight, dpost_bias   out, fp32 [width], any may be NULL; like a [width] dgate they are summed in

@@ -1,5 +1,10 @@
 // Block-sparse product with bias, activation and residual in its epilogue: the kernels of blast_bsr_spmm, whose sums go
-// through an Epilogue (kern_common.h) on the way out.
+// through an Epilogue (kern_common.h) on the way out, which costs the product what its operands' bytes cost: microseconds of the product
+// alone / with bias / SiLU / bf16 residual / Z: 1600 x 6400 at 80 %, 64-wide, 333 tokens 10.6 / 10.5 / 11.1 / 11.2 / 11.2; 2048 x 8192
+// at 90 %, 2048 tokens, fp32 15.6 / 15.6 / 15.7 / 16.2 / 16.6; 14336 x 4096 at 95 %, 128-wide, 4096 tokens, bf16 44.2 / 45.7 / 50.5 / 74.0
+// / 61.5; one token, 6400 x 1600 3.5 whatever is asked for.  Bias and residual are loaded before the waves that share a tile meet
+// (shared tiles, 333 tokens: 17.7 us when they were loaded after, 11.2).  Rows are never cut into chunks: the activation needs complete
+// sums, and the result does not depend on the schedule.
 #include "product_launch.h"
 
 namespace {

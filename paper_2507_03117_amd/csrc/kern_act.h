@@ -3,7 +3,9 @@
 //
 // Bound: memory, every operand read and every result written once.  A workgroup takes 256 columns, eight to a lane (16
 // bytes of bf16), and a run of rows that its eight half-waves deal among themselves; the sums of a lane's columns stay in its
-// registers over the run and meet in LDS at its end.
+// registers over the run and meet in LDS at its end, those of the runs in a second launch - or, for few rows, a workgroup has its
+// columns' rows to the end (k_act_backward_columns).  Measured: gated, 4096 x 14336, fp32 gradient 163 us (5.05 TB/s, the rate of a
+// large copy); GELU with the bias' gradient, 333 x 6400 7.4 us, 4096 x 6400 39 us.
 #pragma once
 #include "kern_rows.h"
 

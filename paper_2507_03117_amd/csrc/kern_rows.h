@@ -20,7 +20,7 @@ __device__ __forceinline__ int piece_at(int c, int j, int lane) {
   return VEC ? (c * NT + lane) * 8 + j : (c * 8 + j) * NT + lane;
 }
 
-// A row of a tensor: the same for all lanes that share it, so that an access is a scalar base and a lane's 32-bit offset.
+// A row of a tensor: where it is the same for all lanes of a wave, an access is a scalar base and a lane's 32-bit offset.
 __device__ __forceinline__ const unsigned char* row_of(const void* base, int64_t at, int bf16) {
   return static_cast<const unsigned char*>(base) + (bf16 ? at * 2 : at * 4);
 }
