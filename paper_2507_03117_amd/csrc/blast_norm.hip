@@ -1,7 +1,9 @@
-// Norms before and after a block with its gate and residual, forward and backward (kern_norm.h).
+// Norms before and after a block with its gate and residual (kern_norm.h): entry points and the forward launches; those of the
+// gradient are in norm_backward.h.
 #include "blast_common.h"
 
 #include "kern_norm.h"
+#include "norm_backward.h"
 
 using namespace blast_dev;
 
@@ -90,106 +92,6 @@ int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
   return launch_forward<16, 4, true>(a, stream);
 }
 
-// Workgroups of a backward pass, each with column sums of its own: one to a row up to kBackwardRows rows, beyond that one of
-// sixteen waves per CU of the full card.  From the sizes alone, so that the workspace does not depend on the device.
-constexpr int kBackwardRows = 512, kBackwardGroups = 256;
-
-// Few rows: the columns have workgroups of their own in the launch of the rows, instead of a second launch that joins the rows'
-// sums, where no other sums are wanted than those of the norm of the stream.
-bool columns_owned(int64_t T, bool branch, int post, bool gate_of_one_row) {
-  return T <= kBackwardRows && (!branch || (!post && !gate_of_one_row));
-}
-
-template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW, bool COLS, bool LAYER, int MODE>
-int launch_backward_m(NormArgs a, hipStream_t stream) {
-  constexpr int kThreads = 64 * NW * TEAMS, kSums = 1 + (MODE >= 1) + LAYER + (LAYER && MODE == 2);
-  constexpr size_t kSumBytes = (size_t)kThreads * NCH * 8 * 4;
-  // sums in LDS: as many as fit, the workgroup having a CU to itself; none where it has one row
-  constexpr int kFit = (int)((size_t)(150 << 10) / kSumBytes), NL = !LOOP ? 0 : kSums < kFit ? kSums : kFit;
-  constexpr size_t kLds = (size_t)NL * kSumBytes;
-  constexpr bool AHEAD = LOOP && ROOM && !(NCH > 1 && LAYER && MODE >= 1);  // (two sums of a layer norm are then in registers)
-  const int64_t rows = (a.T + TEAMS - 1) / TEAMS;
-  int64_t grid = LOOP && rows > kBackwardGroups ? kBackwardGroups : rows;
-  if constexpr (COLS) {
-    if (a.sum_out[0] || a.sum_out[1]) a.column_groups = (a.width + 16 * kNormOwned - 1) / (16 * kNormOwned) * 16;
-    grid += a.column_groups;
-  }
-  constexpr auto kernel = &k_norm_backward<NW, NCH, TEAMS, VEC, LAYER, MODE, NL, LOOP, AHEAD, LOW, COLS>;
-  if constexpr (kLds > 48 * 1024) {
-    static blast::DeviceFlags lds_set;
-    int dev = 0;
-    BLAST_HIP_TRY(hipGetDevice(&dev));
-    if (!lds_set.test(dev)) {
-      BLAST_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
-      lds_set.set(dev);
-    }
-  }
-  kernel<<<dim3((unsigned)grid), dim3(kThreads), kLds, stream>>>(a);
-  BLAST_LAUNCH_CHECK("k_norm_backward");
-  if (COLS || grid == 1) return BLAST_OK;
-  JoinArgs j{};
-  j.part = a.part;
-  j.groups = (int)grid;
-  j.width = a.width;
-  int n = 0;
-  for (int s = 0; s < kNormSums; ++s)
-    if (a.sum_out[s]) j.out[n++] = a.sum_out[s];
-  if (n == 0) return BLAST_OK;
-  k_join_sums<<<dim3((unsigned)((a.width + 63) / 64), (unsigned)n), dim3(1024), 0, stream>>>(j);
-  BLAST_LAUNCH_CHECK("k_join_sums");
-  return BLAST_OK;
-}
-
-template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW, bool LAYER>
-int launch_backward_k(const NormArgs& a, hipStream_t stream) {
-  const int mode = !a.y ? 0 : a.post ? 2 : 1;
-  if constexpr (!LOOP) {
-    if (columns_owned(a.T, a.y != nullptr, a.post, a.gate && a.ldg == 0)) {
-      if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, false, false, LOW, true, LAYER, 0>(a, stream);
-      return launch_backward_m<NW, NCH, TEAMS, VEC, false, false, LOW, true, LAYER, 1>(a, stream);
-    }
-  } else {
-    if (mode == 0) return launch_backward_m<NW, NCH, TEAMS, VEC, true, ROOM, LOW, false, LAYER, 0>(a, stream);
-  }
-  if (mode == 1) return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, LAYER, 1>(a, stream);
-  return launch_backward_m<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false, LAYER, 2>(a, stream);
-}
-
-template <int NW, int NCH, int TEAMS, bool VEC, bool LOOP, bool ROOM, bool LOW = false>
-int launch_backward(const NormArgs& a, hipStream_t stream) {
-  return a.layer ? launch_backward_k<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, true>(a, stream)
-                 : launch_backward_k<NW, NCH, TEAMS, VEC, LOOP, ROOM, LOW, false>(a, stream);
-}
-
-int dispatch_backward(const NormArgs& a, bool vec, hipStream_t stream) {
-  const bool few = a.T <= kBackwardRows;  // a row to a workgroup
-  if (!vec) {
-    if (a.width <= 2048) return few ? launch_backward<4, 1, 1, false, false, false>(a, stream) : launch_backward<4, 1, 1, false, true, false>(a, stream);
-    if (a.width <= 8192) return few ? launch_backward<16, 1, 1, false, false, false>(a, stream) : launch_backward<16, 1, 1, false, true, false>(a, stream);
-    return few ? launch_backward<16, 4, 1, false, false, false>(a, stream) : launch_backward<16, 4, 1, false, true, false>(a, stream);
-  }
-  const bool low = a.h_bf16 && a.dx_bf16 && (!a.w || a.p_bf16) &&
-                   (!a.y || (a.y_bf16 && (!a.dy || a.dy_bf16) && (!a.gate || a.g_bf16) && ((!a.pw && !a.pb) || a.p_bf16)));
-  if (few) {
-    if (a.width <= 512) return launch_backward<1, 1, 1, true, false, false>(a, stream);
-    if (a.width <= 1024) return launch_backward<2, 1, 1, true, false, false>(a, stream);
-    if (a.width <= 2048) return launch_backward<4, 1, 1, true, false, false>(a, stream);
-    if (a.width <= 4096) return launch_backward<8, 1, 1, true, false, false>(a, stream);
-    if (a.width <= 8192) return launch_backward<16, 1, 1, true, false, false>(a, stream);
-    if (a.width <= 16384)
-      return low ? launch_backward<16, 2, 1, true, false, false, true>(a, stream) : launch_backward<16, 2, 1, true, false, false>(a, stream);
-    return launch_backward<16, 4, 1, true, false, false>(a, stream);
-  }
-  if (a.width <= 512) return launch_backward<1, 1, 16, true, true, true>(a, stream);
-  if (a.width <= 1024) return launch_backward<2, 1, 8, true, true, true>(a, stream);
-  if (a.width <= 2048) return launch_backward<4, 1, 4, true, true, true>(a, stream);
-  if (a.width <= 4096) return launch_backward<8, 1, 2, true, true, true>(a, stream);
-  if (a.width <= 8192) return launch_backward<16, 1, 1, true, true, true>(a, stream);
-  if (a.width <= 16384)
-    return low ? launch_backward<16, 2, 1, true, true, true, true>(a, stream) : launch_backward<16, 2, 1, true, true, false>(a, stream);
-  return launch_backward<16, 4, 1, true, true, false>(a, stream);
-}
-
 }  // namespace
 
 extern "C" int blast_norm_residual(const blast_norm_view* P, const void* h, int64_t ldh, int32_t h_dtype, const void* y,
@@ -231,7 +133,9 @@ extern "C" int blast_norm_residual_backward_workspace(const blast_norm_view* P, 
   const int layer = P->kind == BLAST_NORM_LAYER;
   const int sums = 1 + layer + (P->post ? 1 + layer : 0) + (P->gate && P->ldg == 0 ? 1 : 0);
   // (without a branch fewer sums are wanted: the size serves that call as well)
-  *ws_bytes = T <= 1 || columns_owned(T, true, P->post, P->gate && P->ldg == 0) ? 0 : (size_t)sums * (size_t)(T < kBackwardRows ? T : kBackwardRows) * (size_t)P->width * 4;
+  const int64_t groups = T < blast::kBackwardRows ? T : blast::kBackwardRows;
+  const bool owned = T <= 1 || blast::columns_owned(T, true, P->post, P->gate && P->ldg == 0);
+  *ws_bytes = owned ? 0 : (size_t)sums * (size_t)groups * (size_t)P->width * 4;
   return BLAST_OK;
 }
 
@@ -278,7 +182,7 @@ extern "C" int blast_norm_residual_backward(const blast_norm_view* P, const void
   if (!stats || !blast::aligned(stats, 16)) return BLAST_ERR_INVALID_ARG;
   size_t need = 0;
   if (int rc = blast_norm_residual_backward_workspace(P, T, &need)) return rc;
-  if (!branch && columns_owned(T, false, 0, false)) need = 0;
+  if (!branch && blast::columns_owned(T, false, 0, false)) need = 0;
   if (need > 0 && (!ws || ws_bytes < need || !blast::aligned(ws, 16))) return BLAST_ERR_WORKSPACE;
   a.part = static_cast<float*>(ws);
   a.h = h_out;
@@ -308,5 +212,5 @@ extern "C" int blast_norm_residual_backward(const blast_norm_view* P, const void
       vec = vec && pieces_ok(dgate, lddg, P->g_dtype);
     }
   }
-  return dispatch_backward(a, vec, stream);
+  return a.layer ? blast::norm_backward_layer(a, vec, stream) : blast::norm_backward_rms(a, vec, stream);
 }

@@ -60,6 +60,7 @@ struct Epilogue {
 };
 struct NoEpilogue {
   static constexpr bool kOn = false;
+  static constexpr int pairs = 1;
   NoEpilogue from(int64_t) const { return *this; }
 };
 

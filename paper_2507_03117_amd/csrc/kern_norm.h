@@ -10,7 +10,7 @@
 // of a dozen tensors in registers the gradient of 2048 features took 137 registers instead of 98.
 // Measured, GPU time alone (a copy of 1 GB moves 5.0 TB/s, of 64 MB in the last-level cache 7.8): forward, 2048 x 2048, norms on
 // both sides, fp32 stream 11.9 us (4.2 TB/s); 4096 x 4096, bf16 26.0 (5.2); 2048 x 16384, gate per token 65.7 (5.1); one row of 4096
-// 3.0.  Gradient: 2048 x 2048 21.2 us (3.6), 4096 x 4096 49.8 (4.0), 2048 x 16384 118 (4.6), 333 x 1600 6.8, 16 x 4096 3.5.
+// 3.0.  Gradient: 2048 x 2048 20.4 us (3.7), 4096 x 4096 48.8 (4.1), 2048 x 16384 118 (4.6), 333 x 1600 6.8, 16 x 4096 3.5.
 #pragma once
 #include "kern_rows.h"
 
@@ -480,23 +480,68 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
   }
   // ---- the workgroup's column sums, of its teams in order, and what they are the gradients of
   if constexpr (TEAMS > 1) {
+    // four columns to a lane of the first 2 NT (512 features, 4096 rows, against eight to the lanes of one team: 12.7 -> 11.2 us)
+    static_assert(VEC && NCH == 1, "");
     __syncthreads();
-    if (team != 0) return;
+    const int i = threadIdx.x, e = i * 4;
+    if (i >= 2 * NT || e >= E) return;
+    typedef float Four __attribute__((ext_vector_type(4)));
+    Four total[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      total[s] = Four{0.0f, 0.0f, 0.0f, 0.0f};
+      if (!kSum[s]) continue;
+      const Four* q = reinterpret_cast<const Four*>(pool) + (kOrder[s] * 2 + i % 2) * (NT * TEAMS) + i / 2;
+#pragma unroll
+      for (int k = 0; k < TEAMS; ++k) total[s] = k == 0 ? q[0] : total[s] + q[k * NT];
+    }
+    auto four = [&](const void* p, int bf16) {
+      if (bf16) {
+        const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + e);
+        return Four{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                    __uint_as_float(w.y & 0xFFFF0000u)};
+      }
+      return *reinterpret_cast<const Four*>(static_cast<const float*>(p) + e);
+    };
+    float* part = a.part;
+    auto put = [&](float* to, Four v) {
+      if (!to) return;
+      if (gridDim.x == 1) {  // (a caller's array may lie anywhere)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[e + j] = v[j];
+        return;
+      }
+      *reinterpret_cast<Four*>(part + (int64_t)blockIdx.x * E + e) = v;
+      part += (int64_t)gridDim.x * E;
+    };
+    put(a.sum_out[0], total[kDw]);
+    if constexpr (LAYER) put(a.sum_out[1], total[kDx]);
+    if constexpr (MODE >= 1) {
+      if (a.sum_out[2]) {  // gate of one row: post_weight sum(q m) + post_bias sum(q)
+        Four v = MODE == 2 && a.pw ? total[kQm] * four(a.pw, p_bf16) : total[kQm];
+        if constexpr (kSum[kQ])
+          if (a.pb) v += total[kQ] * four(a.pb, p_bf16);
+        put(a.sum_out[2], v);
+      }
+      const bool one_row = a.gate && !per_token;
+      const Four g1 = one_row ? four(a.gate, g_bf16) : Four{1.0f, 1.0f, 1.0f, 1.0f};
+      put(a.sum_out[3], total[kQm] * g1);
+      if constexpr (kSum[kQ]) put(a.sum_out[4], total[kQ] * g1);
+    }
+    return;
   }
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       if (!in_lds(s)) continue;
-#pragma unroll 1
-      for (int k = 0; k < TEAMS; ++k)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const float4 v = *slot(s, c, half, k);
-          const float f[4] = {v.x, v.y, v.z, v.w};
+      for (int half = 0; half < 2; ++half) {
+        const float4 v = *slot(s, c, half, 0);
+        const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) sum[s][c][4 * half + j] = k == 0 ? f[j] : sum[s][c][4 * half + j] + f[j];
-        }
+        for (int j = 0; j < 4; ++j) sum[s][c][4 * half + j] = f[j];
+      }
     }
     float* part = a.part;
     auto put = [&](float* to, const float (&v)[8]) {

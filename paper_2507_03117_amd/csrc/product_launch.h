@@ -36,24 +36,19 @@ int launch_tile(TileArgs a, hipStream_t stream, const EPI& epi = EPI{}) {
   const int64_t grid = (int64_t)a.ntt * a.nbr;
   if (grid <= 0) return BLAST_OK;
   if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
-  static blast::DeviceFlags lds_set;
-  if constexpr (EPI::kOn) {
-    if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, false, false, EPI>), C::LDS_BYTES, lds_set)) return rc;
-    k_spmm_tile<B, false, false, EPI><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, epi);
-  } else {
-    if constexpr (!DUAL) {
-      if (a.act >= 0) {  // single matrix with an activation on the output
-        static blast::DeviceFlags lds_set_post;
-        if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, false, true>), C::LDS_BYTES, lds_set_post))
-          return rc;
-        k_spmm_tile<B, false, true><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, NoEpilogue{});
-        BLAST_LAUNCH_CHECK("k_spmm_tile");
-        return BLAST_OK;
-      }
+  if constexpr (!DUAL && !EPI::kOn) {
+    if (a.act >= 0) {  // single matrix with an activation on the output
+      static blast::DeviceFlags lds_set_post;
+      if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, false, true>), C::LDS_BYTES, lds_set_post))
+        return rc;
+      k_spmm_tile<B, false, true><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, epi);
+      BLAST_LAUNCH_CHECK("k_spmm_tile");
+      return BLAST_OK;
     }
-    if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, DUAL>), C::LDS_BYTES, lds_set)) return rc;
-    k_spmm_tile<B, DUAL><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, NoEpilogue{});
   }
+  static blast::DeviceFlags lds_set;
+  if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(&k_spmm_tile<B, DUAL, false, EPI>), C::LDS_BYTES, lds_set)) return rc;
+  k_spmm_tile<B, DUAL, false, EPI><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a, epi);
   BLAST_LAUNCH_CHECK("k_spmm_tile");
   return BLAST_OK;
 }
@@ -208,20 +203,6 @@ int launch_stream_tw(TileArgs a, const ChunkPlan& plan, int64_t k_features, hipS
   sa.chunk_ke = plan.chunk_ke;
   const int64_t slab = ((int64_t)a.ntt + 7) / 8 * C::TT * k_features * 2;
   const int64_t grid = stream_grid<C, B>(sa, n_rows, cu_count(), slab);
-  if constexpr (EPI::kOn) {
-    auto launch = [&](auto pairs) -> int {
-      constexpr auto kernel = &k_spmm_stream<B, false, TW, false, false, NW, false, false, pairs.value, EPI>;
-      static blast::DeviceFlags lds_set;
-      if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(kernel), C::LDS_BYTES, lds_set)) return rc;
-      kernel<<<dim3((unsigned)grid), dim3(64 * NW), C::LDS_BYTES, stream>>>(sa, epi);
-      BLAST_LAUNCH_CHECK("k_spmm_stream");
-      return BLAST_OK;
-    };
-    if constexpr (C::PAIR)
-      return a.y_pairs && epi.pairs && !(B == 128 && !a.y_bf16) ? launch(std::true_type{}) : launch(std::false_type{});
-    else
-      return launch(std::true_type{});
-  } else {
   if constexpr (LONG) {
     sa.hdr1 = plan.hdr1;
     sa.chunk_row1 = plan.chunk_row1;
@@ -249,27 +230,29 @@ int launch_stream_tw(TileArgs a, const ChunkPlan& plan, int64_t k_features, hipS
     sa.z_T = z.T;
     z.done = true;
   }
-  if (CHUNK && !plan.pre_zeroed) {
-    k_zero_shared_rows<B><<<dim3((unsigned)plan.max_chunks, (unsigned)((a.T + 63) / 64)), dim3(256), 0, stream>>>(sa);
-    BLAST_LAUNCH_CHECK("k_zero_shared_rows");
+  if constexpr (CHUNK) {
+    if (!plan.pre_zeroed) {
+      k_zero_shared_rows<B><<<dim3((unsigned)plan.max_chunks, (unsigned)((a.T + 63) / 64)), dim3(256), 0, stream>>>(sa);
+      BLAST_LAUNCH_CHECK("k_zero_shared_rows");
+    }
   }
   auto launch = [&](auto post, auto pairs) -> int {
-    constexpr auto kernel = &k_spmm_stream<B, DUAL, TW, CHUNK, post.value, NW, LONG, false, pairs.value>;
+    constexpr auto kernel = &k_spmm_stream<B, DUAL, TW, CHUNK, post.value, NW, LONG, false, pairs.value, EPI>;
     static blast::DeviceFlags lds_set;
     if (int rc = ensure_lds_limit(reinterpret_cast<const void*>(kernel), C::LDS_BYTES, lds_set)) return rc;
-    kernel<<<dim3((unsigned)grid), dim3(64 * NW), C::LDS_BYTES, stream>>>(sa, NoEpilogue{});
+    kernel<<<dim3((unsigned)grid), dim3(64 * NW), C::LDS_BYTES, stream>>>(sa, epi);
     BLAST_LAUNCH_CHECK("k_spmm_stream");
     return BLAST_OK;
   };
-  if constexpr (!DUAL && !CHUNK && !LONG) {
+  if constexpr (!DUAL && !CHUNK && !LONG && !EPI::kOn) {
     // single matrix with an activation on the output: the intermediate of a two-matrix MLP, which takes row pairs
     if (a.act >= 0) return launch(std::true_type{}, std::true_type{});
   }
   int rc;
   if constexpr (C::PAIR && !CHUNK && !LONG)
-    // Two rows to a store: only where Y allows it, and with 128-wide blocks not in fp32, where whole lines leave either way (14336
+    // Two rows to a store: only where Y (and what an epilogue reads and keeps) allows it, and with 128-wide blocks not in fp32, where whole lines leave either way (14336
     // x 4096 at 90 %, pairs / neighbouring rows, 512 tokens 19.4 / 18.9 us, 2048: 46.0 / 45.0; 53248 x 16384 at 95 %, 300: 64.2 / 62.5).
-    rc = a.y_fast && a.y_pairs && !(B == 128 && !a.y_bf16) ? launch(std::false_type{}, std::true_type{}) : launch(std::false_type{}, std::false_type{});
+    rc = a.y_fast && a.y_pairs && epi.pairs && !(B == 128 && !a.y_bf16) ? launch(std::false_type{}, std::true_type{}) : launch(std::false_type{}, std::false_type{});
   else
     rc = launch(std::false_type{}, std::true_type{});
   if (rc) return rc;
@@ -280,7 +263,6 @@ int launch_stream_tw(TileArgs a, const ChunkPlan& plan, int64_t k_features, hipS
     BLAST_LAUNCH_CHECK("k_long_finish");
   }
   return BLAST_OK;
-  }
 }
 
 template <int B, bool DUAL, bool CHUNK, class EPI = NoEpilogue>
