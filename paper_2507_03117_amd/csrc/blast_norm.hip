@@ -122,6 +122,7 @@ extern "C" int blast_norm_residual(const blast_norm_view* P, const void* h, int6
     a.y_bf16 = y_dtype == BLAST_BF16;
     a.h_out = h_out;
     a.ldho = ldho;
+    a.past = T * P->width * (a.h_bf16 ? 2 : 4) >= kPastBytes;
     vec = vec && pieces_ok(y, ldy, y_dtype) && pieces_ok(h_out, ldho, h_dtype);
   }
   return dispatch_forward(a, vec, stream);

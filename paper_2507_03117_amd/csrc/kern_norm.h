@@ -9,7 +9,7 @@
 // 13.2 / 13.8 us, 1600 features, 333 rows 3.7 / 4.7.  Row addresses are scalar with one 32-bit offset a lane: with 64-bit addresses
 // of a dozen tensors in registers the gradient of 2048 features took 137 registers instead of 98.
 // Measured, GPU time alone (a copy of 1 GB moves 5.0 TB/s, of 64 MB in the last-level cache 7.8): forward, 2048 x 2048, norms on
-// both sides, fp32 stream 11.9 us (4.2 TB/s); 4096 x 4096, bf16 26.0 (5.2); 2048 x 16384, gate per token 65.7 (5.1); one row of 4096
+// both sides, fp32 stream 11.9 us (4.2 TB/s); 4096 x 4096, bf16 24.3 (5.5); 2048 x 16384, gate per token 66.6 (5.0); one row of 4096
 // 3.0.  Gradient: 2048 x 2048 20.4 us (3.7), 4096 x 4096 48.8 (4.1), 2048 x 16384 118 (4.6), 333 x 1600 6.8, 16 x 4096 3.5.
 #pragma once
 #include "kern_rows.h"
@@ -30,7 +30,14 @@ struct NormArgs {
   int layer, post;
   float eps, scale;
   int column_groups;  // workgroups of a gradient launch that own columns (see norm_columns)
+  int past;  // the stream's new values leave past the L2
 };
+
+// A stream of this size or more is written past the L2s (4 MB each, 32 together), which it would only empty: it is read again after
+// the block's products.  4096 x 4096 bf16 26.2 -> 24.3 us, 2048 x 8192 31.7 -> 27.9, 2048 x 12000 fp32 107.5 -> 97.5, 2048 x 16384
+// with a gate per token 66.3 -> 66.6; the step, two products and the next step with 4096 x 4096 141 -> 139.  Smaller streams gain alone
+// (2048 x 4096 bf16 13.2 -> 12.4) and lose in that chain (78.6 -> 82.0), as x and the gradients do, which the next launch reads.
+constexpr int64_t kPastBytes = 32 << 20;
 
 constexpr int kNormSums = 5;
 
@@ -133,7 +140,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void k_norm_residual(const
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[c][j] = __builtin_fmaf(a.scale, p[c][j], v[c][j]);
-        piece_store<NT, VEC>(row_of(a.h_out, t * a.ldho, h_bf16), c, lane, E, h_bf16, v[c]);
+        unsigned char* to = row_of(a.h_out, t * a.ldho, h_bf16);
+        if (a.past)
+          piece_store<NT, VEC, true>(to, c, lane, E, h_bf16, v[c]);
+        else
+          piece_store<NT, VEC>(to, c, lane, E, h_bf16, v[c]);
       }
       if (more) ask(g, a.gate, (t + step) * a.ldg, g_bf16, false);
     } else {

@@ -77,18 +77,26 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return (uint32_t)f32_to_bf16_rne(a) | ((uint32_t)f32_to_bf16_rne(b) << 16);
 }
 
-template <int NT, bool VEC>
+// PAST: the result leaves past the L2 (see kPastBytes).
+template <int NT, bool VEC, bool PAST = false>
 __device__ __forceinline__ void piece_store(unsigned char* row, int c, int lane, int width, int bf16, const float (&v)[8]) {
   if constexpr (VEC) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    auto put = [](auto* p, auto x) {
+      if constexpr (PAST)
+        __builtin_nontemporal_store(x, p);
+      else
+        *p = x;
+    };
     const uint32_t e = (uint32_t)(c * NT + lane) * 8;
     if (e < (uint32_t)width) {
       if (bf16) {
-        *reinterpret_cast<u32x4*>(row + e * 2) =
-            u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+        put(reinterpret_cast<u32x4*>(row + e * 2),
+            u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])});
       } else {
-        float4* p = reinterpret_cast<float4*>(row + e * 4);
-        p[0] = float4{v[0], v[1], v[2], v[3]};
-        p[1] = float4{v[4], v[5], v[6], v[7]};
+        f32x4* p = reinterpret_cast<f32x4*>(row + e * 4);
+        put(p, f32x4{v[0], v[1], v[2], v[3]});
+        put(p + 1, f32x4{v[4], v[5], v[6], v[7]});
       }
     }
   } else {
