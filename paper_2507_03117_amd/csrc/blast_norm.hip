@@ -59,6 +59,23 @@ bool params_pieces_ok(const NormArgs& a) {
          blast::aligned(a.pb, 16) && pieces_ok(a.gate, a.ldg, a.g_bf16 ? BLAST_BF16 : BLAST_F32);
 }
 
+const void* row_at(const void* p, int64_t at, int bf16) { return static_cast<const char*>(p) + at * (bf16 ? 2 : 4); }
+void* row_at(void* p, int64_t at, int bf16) { return static_cast<char*>(p) + at * (bf16 ? 2 : 4); }
+
+// The call without its first n rows.
+NormArgs rows_after(NormArgs a, int64_t n) {
+  a.T -= n;
+  a.h = row_at(a.h, n * a.ldh, a.h_bf16);
+  a.x = row_at(a.x, n * a.ldx, a.x_bf16);
+  if (a.y) {
+    a.y = row_at(a.y, n * a.ldy, a.y_bf16);
+    a.h_out = row_at(a.h_out, n * a.ldho, a.h_bf16);
+    if (a.gate) a.gate = row_at(a.gate, n * a.ldg, a.g_bf16);
+  }
+  if (a.stats) a.stats += n * 4;
+  return a;
+}
+
 // A row (with one wave to a row, four) to a workgroup while several workgroups fit on a CU: the others' loads cover one's
 // sums (16 waves a CU that go over the rows, one ahead / a row each, microseconds: 4096 x 4096, branch with a norm 29.8 / 26.0; 2048
 // x 8192 33.3 / 31.1; one row of 4096 3.5 / 3.0).  Rows of more than 8192 take a CU for themselves: a workgroup per CU goes over them, one
@@ -66,8 +83,15 @@ bool params_pieces_ok(const NormArgs& a) {
 template <int NW, int NCH, bool VEC, bool AHEAD = false, bool LOW = false>
 int launch_forward(const NormArgs& a, hipStream_t stream) {
   constexpr int kRows = NW == 1 ? 4 : 1;
-  int64_t grid = (a.T + kRows - 1) / kRows;
   constexpr int kThreads = NW == 1 ? 256 : 64 * NW;
+  constexpr int64_t kMostRows = ((int64_t)1 << 31) / kThreads * kRows;  // of a launch (fewer than 2^32 lanes)
+  if (NW * NCH <= 16 && a.T > kMostRows) {
+    NormArgs part = a;
+    part.T = kMostRows;
+    if (int rc = launch_forward<NW, NCH, VEC, AHEAD, LOW>(part, stream)) return rc;
+    return launch_forward<NW, NCH, VEC, AHEAD, LOW>(rows_after(a, kMostRows), stream);
+  }
+  const int64_t grid = (a.T + kRows - 1) / kRows;
   if (NW * NCH > 16 && grid > 256) {
     k_norm_residual<NW, NCH, VEC, (NW * NCH > 16), AHEAD, LOW><<<dim3(256), dim3(kThreads), 0, stream>>>(a);
   } else {

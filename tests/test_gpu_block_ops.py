@@ -474,6 +474,27 @@ def test_norm_pitches_and_places(E):
     check_forward(s, "in place", h=stream, h_out=stream)
 
 
+@pytest.mark.parametrize("T,E,h,gate,cuts", [(4100, 4096, "bf16", None, (0, 7, 2000, 4100)), (1030, 16384, "bf16", "tokens", (0, 300, 301, 1030)),
+                                             (2050, 8200, "f32", "vector", (0, 1000, 2050)),
+                                             (2 ** 26 + 5, 8, "bf16", "tokens", (0, 2 ** 25, 2 ** 25 + 1, 2 ** 26 + 5))])
+def test_norm_of_many_rows_is_that_of_its_parts(T, E, h, gate, cuts):
+    """Streams beyond the L2s, and more rows than a launch has lanes for: bit for bit what calls on runs of the rows give, one
+    run of which is held against the definition."""
+    g = torch.Generator(device=DEV).manual_seed(T)
+    make = lambda *shape, dtype=torch.bfloat16: torch.randn(shape, generator=g, device=DEV, dtype=dtype)
+    hd, yd, w = make(T, E, dtype=TYPES[h]), make(T, E), make(E)
+    gd = None if gate is None else make(T, E) if gate == "tokens" else make(E)
+    part = lambda t, a, b: t if t is None or t.dim() == 1 else t[a:b]
+    new_h, x, stats = api.norm_residual(hd, yd, weight=w, gate=gd, scale=0.5, with_stats=True)
+    for a, b in zip(cuts, cuts[1:]):
+        ph, px, ps = api.norm_residual(hd[a:b], yd[a:b], weight=w, gate=part(gd, a, b), scale=0.5, with_stats=True)
+        assert torch.equal(ph, new_h[a:b]) and torch.equal(px, x[a:b]) and torch.equal(ps, stats[a:b])
+    a = T - 5
+    args = dict(norm_inputs(1, 5, E, "rms")["args"], weight=w.cpu(), gate=None if gd is None else part(gd, a, T).cpu(), scale=0.5)
+    check_forward(dict(h=hd[a:].cpu(), y=yd[a:].cpu(), args=args), h=hd[a:].clone(), y=yd[a:].clone())
+    assert torch.equal(api.norm_residual(hd[a:], yd[a:], **on_gpu(args))[1], x[a:])
+
+
 def test_norm_hard_rows():
     """Rows whose mean is far from their deviation, constant rows, rows of zeros; one row's infinity or NaN stays in it."""
     T, E = 8, 1600
