@@ -111,7 +111,8 @@ int dispatch_forward(const NormArgs& a, bool vec, hipStream_t stream) {
   if (a.width <= 2048) return launch_forward<4, 1, true>(a, stream);
   if (a.width <= 4096) return launch_forward<8, 1, true>(a, stream);
   if (a.width <= 8192) return launch_forward<16, 1, true>(a, stream);
-  const bool low = a.h_bf16 && (!a.w || a.p_bf16) && (!a.y || (a.y_bf16 && (!a.gate || a.g_bf16) && ((!a.pw && !a.pb) || a.p_bf16)));
+  // (every operand that the kernel converts: a weight or a bias may be there without the other, and pw, pb are null without a branch)
+  const bool low = a.h_bf16 && ((!a.w && !a.b && !a.pw && !a.pb) || a.p_bf16) && (!a.y || (a.y_bf16 && (!a.gate || a.g_bf16)));
   if (a.width <= 16384) return low ? launch_forward<16, 2, true, true, true>(a, stream) : launch_forward<16, 2, true>(a, stream);
   return launch_forward<16, 4, true>(a, stream);
 }
