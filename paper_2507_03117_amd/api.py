@@ -819,10 +819,13 @@ def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats
                            gate: Optional[torch.Tensor] = None, scale: float = 1.0, eps: float = 1e-5,
                            dy_dtype: torch.dtype = torch.bfloat16, dh: Optional[torch.Tensor] = None) -> NormGrads:
     """blast_norm_residual_backward.  h_out, stats: of the forward call; dx: gradient of x; dh_out: of h_out through the rest of
-    the stream; dh: where the gradient of h goes (it may be dh_out)."""
+    the stream; dh: where the gradient of h goes (it may be dh_out).  A [T, width] gate whose tokens share one row of memory
+    (Tensor.expand) has a gradient per token like any other and is copied for it; pass the [width] row for their sum."""
     L = lib()
     assert h_out.dim() == 2
     T, E = h_out.shape
+    if gate is not None and y is not None and gate.dim() == 2 and T > 1 and gate.stride(0) == 0:
+        gate = gate.contiguous()  # (to the C call a pitch of 0 is a gate of one row, whose gradient is a sum)
     shape, h_dtype = h_out.shape, h_out.dtype
     v = _norm_view(E, T, kind, weight, bias, post, post_weight, post_bias, gate, scale, eps)
     branch, same = y is not None, (h_dtype,)

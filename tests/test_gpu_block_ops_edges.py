@@ -1,4 +1,4 @@
-"""Edges of the operators around the MLP: parameters that come alone.
+"""Edges of the operators around the MLP: parameters that come alone, gates laid out by a stride of 0.
 
 Definitions and tolerances are those of test_gpu_block_ops.py; the ones of this file are derived where they stand.  Inputs of the large
 cases are made, and compared in 64 bits, on the card."""
@@ -60,3 +60,16 @@ def test_norm_with_one_parameter(on_card, E, T):
                         s["args"][k] = None
                 ops.check_forward(s, f"{keep} {params} {y} {post}")
                 ops.check_backward(s, f"{keep} {params} {y} {post}")
+
+
+@pytest.mark.parametrize("T", [1, 2, 6, 600])
+@pytest.mark.parametrize("kind,post", [("rms", False), ("layer", True)])
+def test_norm_gate_of_one_row_for_all_tokens_by_its_strides(on_card, T, kind, post):
+    """A [T, width] gate whose rows are one row in memory: its gradient is that of the same gate with rows of its own."""
+    for params, E in (("bf16", 72), ("f32", 131), ("bf16", 2048)):
+        s = norm_inputs(T + E, T, E, kind, "bf16", "bf16", params, post, "vector", 0.7)
+        s["args"]["gate"] = s["args"]["gate"].expand(T, E)
+        ops.check_forward(s, f"{E} {params}")
+        ops.check_backward(s, f"{E} {params}")
+        s["args"]["gate"] = s["args"]["gate"][:1].clone().expand(T, E)
+        ops.check_backward(s, f"{E} {params}, one row expanded")
