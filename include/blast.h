@@ -503,7 +503,8 @@ int blast_bsr_gated_spmm(const blast_bsr_view* Wgate, const blast_bsr_view* Wup,
  *   W, X, ldx, layout, T     as in blast_bsr_spmm (W->aux is not read: rows are never cut into chunks, so sums have a fixed
  *                            order)
  *   bias                     fp32 [rows], may be NULL
- *   act                      BLAST_ACT_NONE, _SILU, _GELU or _RELU
+ *   act                      BLAST_ACT_NONE, _SILU, _GELU or _RELU (a NaN stays one; in the other products of this file ReLU
+ *                            makes it 0)
  *   R, ldr, r_dtype          residual in the layout of X, fp32 or bf16, may be NULL; may be Y itself (same pitch and type)
  *   Y, ldy, y_dtype          out, in the layout of X, fp32 or bf16
  *   Z, ldz                   out, bf16 in the layout of X, may be NULL: what blast_act_backward reads; overlaps neither Y nor R
@@ -521,7 +522,8 @@ int blast_bsr_linear(const blast_bsr_view* W, const uint16_t* X, int64_t ldx, in
  *     gated:            H = act(Z) U,  dZ = dY U act'(Z),  dU = dY act(Z),  dbias_z = sum_t dZ,  dbias_u = sum_t dU
  * (the first half of Eq. (1) with Z = Wgate X, dY the gradient of H; H is what the gradient of Wdown needs, made again
  * instead of kept).  All tensors token-major [T][N].  fp32 arithmetic, one rounding when a value is stored; the sums are of
- * the unrounded values, in fp32 and in a fixed order.  relu'(0) = 0.
+ * the unrounded values, in fp32 and in a fixed order.  relu'(0) = 0; a NaN in Z
+ * enters dU and H through every activation, and relu' of it is 0.
  *   Z, ldz            bf16; may be NULL with BLAST_ACT_NONE and no U (only dY is read then)
  *   U, ldu            bf16 or NULL
  *   dY, lddy, dy_dtype   fp32 or bf16

@@ -36,7 +36,7 @@ __device__ __forceinline__ void act_and_slope(int act, float z, float& a, float&
     a = gelu(z);
   } else if (act == BLAST_ACT_RELU) {
     s = z > 0.0f ? 1.0f : 0.0f;
-    a = z > 0.0f ? z : 0.0f;
+    a = z <= 0.0f ? 0.0f : z;  // (a NaN stays one)
   } else {
     s = 1.0f;
     a = z;

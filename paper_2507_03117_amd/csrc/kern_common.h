@@ -136,6 +136,12 @@ __device__ __forceinline__ float apply_act(int act, float g) {
   return g > 0.0f ? g : 0.0f;
 }
 
+// Activation in an Epilogue: post_act, but a NaN stays one through ReLU (the products above make it 0, as their oracle does).
+__device__ __forceinline__ float epilogue_act(int act, float v) {
+  if (act == BLAST_ACT_RELU) return v <= 0.0f ? 0.0f : v;
+  return post_act(act, v);
+}
+
 __device__ __forceinline__ float bf16_value(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
 // N neighbouring rows' values (N = 1, 2, 4) of one token's residual and of the bias, asked for before they are needed: rows are
@@ -205,7 +211,7 @@ __device__ __forceinline__ void epilogue_apply(const Epilogue& e, const Epilogue
   }
   if (e.act >= 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = post_act(e.act, v[i]);
+    for (int i = 0; i < N; ++i) v[i] = epilogue_act(e.act, v[i]);
   }
   if (e.R) {
     if (N > 1 && e.r_bf16 && wide) {
@@ -222,7 +228,7 @@ __device__ __forceinline__ void epilogue_apply(const Epilogue& e, const Epilogue
 __device__ __forceinline__ float epilogue_value(const Epilogue& e, float v, int64_t tok, int64_t row) {
   if (e.bias) v += e.bias[row];
   if (e.Z) e.Z[tok * e.szt + row * e.szi] = f32_to_bf16_rne(v);
-  if (e.act >= 0) v = post_act(e.act, v);
+  if (e.act >= 0) v = epilogue_act(e.act, v);
   if (e.R) {
     const int64_t at = tok * e.srt + row * e.sri;
     v += e.r_bf16 ? bf16_value(static_cast<const uint16_t*>(e.R)[at]) : static_cast<const float*>(e.R)[at];

@@ -499,7 +499,7 @@ __device__ __forceinline__ void stream_epilogue(const Epilogue& e, f32x16 (&acc)
 #pragma unroll
         for (int ni = 0; ni < C::NI; ++ni)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) acc[mi][ni][j] = post_act(act.value, acc[mi][ni][j]);
+          for (int j = 0; j < 16; ++j) acc[mi][ni][j] = epilogue_act(act.value, acc[mi][ni][j]);
     };
     // the branch on the activation stays outside the unrolled loops: one copy of each function body
     if (e.act == BLAST_ACT_GELU)

@@ -1,4 +1,4 @@
-"""Edges of the operators around the MLP: parameters that come alone, gates laid out by a stride of 0.
+"""Edges of the operators around the MLP: parameters that come alone, gates laid out by a stride of 0, NaN before a ReLU.
 
 Definitions and tolerances are those of test_gpu_block_ops.py; the ones of this file are derived where they stand.  Inputs of the large
 cases are made, and compared in 64 bits, on the card."""
@@ -73,3 +73,49 @@ def test_norm_gate_of_one_row_for_all_tokens_by_its_strides(on_card, T, kind, po
         ops.check_backward(s, f"{E} {params}")
         s["args"]["gate"] = s["args"]["gate"][:1].clone().expand(T, E)
         ops.check_backward(s, f"{E} {params}, one row expanded")
+
+
+def test_linear_keeps_nan_before_a_relu():
+    """A NaN sum stays NaN through every activation, in every kernel; the other rows are as without it."""
+    for b in (16, 32, 64, 128):
+        packed, dense = ops.matrix(b, 4 * b, 3 * b, b, 0.6)
+        rows, cols = dense.shape
+        bias = ops.rand(1, (rows,)).to(DEV)
+        bad = bias.clone()
+        bad[5], bad[rows - 1] = float("nan"), float("nan")
+        for T in (1, 20, 40, 300, 1030):
+            x = ops.rand(T, (T, cols), torch.bfloat16).to(DEV)
+            for act in ("relu", "gelu", "silu"):
+                for layout in (api.TOKEN_MAJOR, api.FEATURE_MAJOR):
+                    xl = x if layout == api.TOKEN_MAJOR else torch.empty((cols, T), dtype=x.dtype, device=DEV).copy_(x.t())
+                    for out in (torch.float32, torch.bfloat16):
+                        call = lambda v: api.bsr_linear(packed, xl, bias=v, act=act, layout=layout, out_dtype=out)  # noqa: E731
+                        got, want = call(bad), call(bias).clone()
+                        if layout == api.FEATURE_MAJOR:
+                            got, want = got.t(), want.t()
+                        assert torch.isnan(got[:, 5]).all() and torch.isnan(got[:, -1]).all(), (b, T, act, layout)
+                        want[:, 5], want[:, -1] = float("nan"), float("nan")
+                        assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want)), (b, T, act, layout)
+
+
+@pytest.mark.parametrize("T", [1, 70, 700])
+def test_act_backward_keeps_nan(T):
+    """What the activation of a NaN enters is NaN; relu' of it is 0, as of everything that is not positive."""
+    N = 264
+    z, u = ops.rand(1, (T, N), torch.bfloat16).to(DEV), ops.rand(2, (T, N), torch.bfloat16).to(DEV)
+    dy = ops.rand(3, (T, N)).to(DEV)
+    bad = z.clone()
+    bad[T - 1, 17], bad[0, 263] = float("nan"), float("nan")
+    at = torch.isnan(bad)
+    for act in ("relu", "gelu", "silu"):
+        for sums in (False, True):
+            clean, got = (api.gated_act_backward(v, u, dy, act=act, bias_grad=sums) for v in (z, bad))
+            for k in ("dU", "H", "dG"):
+                g, c = getattr(got, k), getattr(clean, k)
+                assert torch.equal(g[~at], c[~at]), (act, k)
+                if act == "relu" and k == "dG":
+                    assert not g[at].any()
+                else:
+                    assert torch.isnan(g[at]).all(), (act, k)
+            one = api.act_backward(bad, dy, act=act, bias_grad=sums)
+            assert torch.isnan(one.dZ[at]).all() if act != "relu" else not one.dZ[at].any()
