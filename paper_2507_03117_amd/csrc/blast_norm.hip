@@ -159,7 +159,7 @@ extern "C" int blast_norm_residual_backward_workspace(const blast_norm_view* P, 
   const int layer = P->kind == BLAST_NORM_LAYER;
   const int sums = 1 + layer + (P->post ? 1 + layer : 0) + (P->gate && P->ldg == 0 ? 1 : 0);
   // (without a branch fewer sums are wanted: the size serves that call as well)
-  const int64_t groups = T < blast::kBackwardRows ? T : blast::kBackwardRows;
+  const int64_t groups = T <= blast::kBackwardRows ? T : blast::kBackwardGroups;
   const bool owned = T <= 1 || blast::columns_owned(T, true, P->post, P->gate && P->ldg == 0);
   *ws_bytes = owned ? 0 : (size_t)sums * (size_t)groups * (size_t)P->width * 4;
   return BLAST_OK;
