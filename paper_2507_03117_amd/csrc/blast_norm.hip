@@ -173,7 +173,7 @@ extern "C" int blast_norm_residual_backward(const blast_norm_view* P, const void
                                             float* dpost_bias, void* ws, size_t ws_bytes, void* stream_) {
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   // (over no rows the operands may be null, so the branch then goes by what is asked for)
-  const bool branch = y != nullptr || (T == 0 && (dgate || dpost_weight || dpost_bias));
+  const bool branch = y != nullptr || (T == 0 && (dy || dgate || dpost_weight || dpost_bias));
   if (int rc = check_norm(P, branch)) return rc;
   if (T < 0 || T > INT32_MAX / 2) return BLAST_ERR_INVALID_ARG;
   if (!dtype_ok(h_dtype) || !dtype_ok(dx_dtype)) return BLAST_ERR_INVALID_ARG;

@@ -22,3 +22,13 @@ def test_norm_backward_workspace_is_what_a_launch_fills(width):
         if sums > 1:  # (a single norm's sums need none up to 512 rows)
             assert norm_workspace(v, 300) == sums * 300 * width * 4 and norm_workspace(v, 512) == sums * 512 * width * 4
         assert norm_workspace(v, 1) == 0
+
+
+def test_norm_backward_over_no_rows_needs_no_operands():
+    """Operands of no rows may be null while outputs are not, the gradient of the branch among them."""
+    none = dict(T=0, h=None, y=None, stats=None, dx=None, dh=None)
+    for v in (view(), view(kind=1), view(post=1), view(gate=P, ldg=64)):
+        assert backward(v, **none) == 0 and backward(v, dy=P, **none) == 0
+    assert backward(view(gate=P, ldg=64), dy=P, dg=P, **none) == 0
+    assert backward(view(), dg=P, **none) == -1  # no gate
+    assert backward(view(), dy=P, **dict(none, T=4)) == -1
