@@ -24,13 +24,14 @@ int64_t run_rows(int64_t T, int64_t N) {
 // A workgroup owns its columns' sums up to this many rows, instead of a second launch that joins runs of rows: that launch and
 // the gap before it take longer than the fewer workgroups lose.  GPU time alone from a graph, owned / joined, microseconds: GELU,
 // 6400 columns, 64 rows 4.5 / 5.6, 333: 7.3 / 8.2, 512: 9.5 / 10.1, 1000: 13.5 / 13.3; two sums (more registers, fewer waves),
-// 6400 columns, 64 rows 6.1 / 6.2, 128: 8.3 / 7.1; a call that waits for the launches saves another 3 to 5.
-bool columns_owned(int64_t T, int wanted) { return T <= (wanted > 1 ? 64 : 512); }
+// 6400 columns, 64 rows 6.1 / 6.2, 128: 8.3 / 7.1; a call that waits for the launches saves another 3 to 5.  Not beyond 2^27 columns,
+// whose owners (32 lanes to a column) would be 2^32 lanes: no launch has as many, and so many columns have their rows in one run.
+bool columns_owned(int64_t T, int64_t N, int wanted) { return T <= (wanted > 1 ? 64 : 512) && N < ((int64_t)1 << 27) - 512; }
 
 template <bool GATED, bool SUMS>
 int launch(const ActArgs& a, bool vec, hipStream_t stream) {
   if constexpr (SUMS) {
-    if (columns_owned(a.T, (a.sum_out[0] ? 1 : 0) + (a.sum_out[1] ? 1 : 0))) {
+    if (columns_owned(a.T, a.N, (a.sum_out[0] ? 1 : 0) + (a.sum_out[1] ? 1 : 0))) {
       const dim3 grid((unsigned)(((int64_t)a.N + 16 * kActOwned - 1) / (16 * kActOwned) * 16));
       if (a.T <= 64) {
         if (vec)
@@ -75,7 +76,7 @@ extern "C" int blast_act_backward_workspace(int64_t T, int64_t N, int32_t n_bias
   *ws_bytes = 0;
   if (T == 0 || N == 0) return BLAST_OK;
   const int64_t rows = run_rows(T, N), runs = (T + rows - 1) / rows;
-  if (runs > 1 && !columns_owned(T, n_bias_grads)) *ws_bytes = (size_t)n_bias_grads * (size_t)runs * (size_t)N * 4;
+  if (runs > 1 && !columns_owned(T, N, n_bias_grads)) *ws_bytes = (size_t)n_bias_grads * (size_t)runs * (size_t)N * 4;
   return BLAST_OK;
 }
 

@@ -1,4 +1,5 @@
-"""Edges of the operators around the MLP: parameters that come alone, gates laid out by a stride of 0, NaN before a ReLU.
+"""Edges of the operators around the MLP: parameters that come alone, gates laid out by a stride of 0, NaN before a ReLU, more
+columns than a launch has owners for.
 
 Definitions and tolerances are those of test_gpu_block_ops.py; the ones of this file are derived where they stand.  Inputs of the large
 cases are made, and compared in 64 bits, on the card."""
@@ -119,3 +120,16 @@ def test_act_backward_keeps_nan(T):
                     assert torch.isnan(g[at]).all(), (act, k)
             one = api.act_backward(bad, dy, act=act, bias_grad=sums)
             assert torch.isnan(one.dZ[at]).all() if act != "relu" else not one.dZ[at].any()
+
+
+@pytest.mark.parametrize("T,N", [(1, (1 << 29) + 72), (65, (1 << 27) + 72)])
+def test_act_backward_sums_of_more_columns_than_a_launch_has_owners(T, N):
+    """The gradient of a bias alone: small whole numbers, whose sums are exact."""
+    dy = torch.randint(-3, 4, (1, N), generator=torch.Generator(DEV).manual_seed(T), device=DEV, dtype=torch.int8)
+    want = dy[0].float() * (1 if T == 1 else T - 2)  # (of T rows one is taken away again)
+    dy = dy.bfloat16().repeat(T, 1)
+    if T > 1:
+        dy[T // 2] *= -1
+    got = torch.full((N,), float("nan"), device=DEV)
+    api._act_backward(None, None, dy, None, None, None, None, got, None)
+    assert torch.equal(got, want)
