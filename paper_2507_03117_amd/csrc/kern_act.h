@@ -14,7 +14,7 @@ namespace blast_dev {
 struct ActArgs {
   const void *z, *u, *dy;
   void *dz, *du, *h;
-  float* part;         // [sum][run][N]; with one run the sums themselves
+  float* part;         // [sum wanted][run][N] (a single run writes sum_out instead)
   float* sum_out[2];   // of dZ, of dU (null: not wanted)
   int64_t ldz, ldu, lddy, lddz, lddu, ldh;
   int T, N, run;       // run: rows of a workgroup

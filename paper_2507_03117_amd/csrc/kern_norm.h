@@ -21,7 +21,7 @@ struct NormArgs {
   const float* stats_in;
   void *h_out, *x, *dh, *dy, *dgate;
   float* stats;
-  float* part;  // column sums of the workgroups, [sum][workgroup][width]; with one workgroup the sums themselves
+  float* part;  // column sums of the workgroups, [sum wanted][workgroup][width] (one workgroup writes sum_out instead)
   float* sum_out[5];  // dweight, dbias, dgate of one row, dpost_weight, dpost_bias (null: not wanted)
   int64_t ldh, ldy, ldg, ldho, ldx, lddx, lddh_in, lddh, lddy, lddg;
   int64_t T;
@@ -491,7 +491,8 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
   }
   // ---- the workgroup's column sums, of its teams in order, and what they are the gradients of
   if constexpr (TEAMS > 1) {
-    // four columns to a lane of the first 2 NT (512 features, 4096 rows, against eight to the lanes of one team: 12.7 -> 11.2 us)
+    // Four columns to a lane of the first 2 NT (512 features, 4096 rows, against eight to the lanes of one team: 12.7 -> 11.2 us).
+    // More than kBackwardRows rows: there is never a single workgroup here.
     static_assert(VEC && NCH == 1, "");
     __syncthreads();
     const int i = threadIdx.x, e = i * 4;
@@ -517,11 +518,6 @@ __global__ __launch_bounds__(64 * NW * TEAMS) void k_norm_backward(const NormArg
     float* part = a.part;
     auto put = [&](float* to, Four v) {
       if (!to) return;
-      if (gridDim.x == 1) {  // (a caller's array may lie anywhere)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) to[e + j] = v[j];
-        return;
-      }
       *reinterpret_cast<Four*>(part + (int64_t)blockIdx.x * E + e) = v;
       part += (int64_t)gridDim.x * E;
     };
