@@ -6,11 +6,12 @@
 // registers of NW waves, NCH pieces of eight values to a lane, so that the variance is taken of the centred values without a second
 // read; sums over a row are DPP steps and, for NW > 1, one barrier.  With NW = 1 a forward workgroup's four waves have a row each
 // and no barrier.  Why one piece a lane up to 8192 features: four waves of one piece against two of two, 2048 features, 4096 rows
-// 13.2 / 13.8 us, 1600 features, 333 rows 3.7 / 4.7.  Row addresses are scalar with one 32-bit offset a lane: with 64-bit addresses
-// of a dozen tensors in registers the gradient of 2048 features took 137 registers instead of 98.
-// Measured, GPU time alone (a copy of 1 GB moves 5.0 TB/s, of 64 MB in the last-level cache 7.8): forward, 2048 x 2048, norms on
-// both sides, fp32 stream 11.9 us (4.2 TB/s); 4096 x 4096, bf16 24.3 (5.5); 2048 x 16384, gate per token 66.6 (5.0); one row of 4096
-// 3.0.  Gradient: 2048 x 2048 20.4 us (3.7), 4096 x 4096 48.8 (4.1), 2048 x 16384 118 (4.6), 333 x 1600 6.8, 16 x 4096 3.5.
+// 13.2 / 13.8 us, forward, 1600 features, 333 rows 3.7 / 4.7.  Row addresses are scalar with one 32-bit offset a lane: 64-bit addresses
+// of a dozen tensors took 39 registers more (the gradient of 2048 features, RMS on both sides, has 107).
+// Measured, a launch among others in a recorded graph (by itself in a kernel trace it takes 0.5 to 1 us more; a copy of 1 GB moves
+// 5.0 TB/s, of 64 MB in the last-level cache 7.8): forward, 2048 x 2048, norms on both sides, fp32 stream 11.9 us (4.2 TB/s); 4096 x
+// 4096, bf16 24.3 (5.5); 2048 x 16384, gate per token 66.6 (5.0); 333 x 1600 3.7; one row of 4096, in a trace 2.9.  Gradient, with
+// the launch that joins the sums: 2048 x 2048 20.1 us (3.8), 4096 x 4096 48.8 (4.1), 2048 x 16384 118 (4.6), 333 x 1600 6.8, 16 x 4096 3.5.
 #pragma once
 #include "kern_rows.h"
 

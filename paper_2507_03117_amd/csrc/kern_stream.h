@@ -996,13 +996,17 @@ __global__ __launch_bounds__(64 * NW, (StreamCfg<B, TW, NW, F8>::WAVES_PER_SIMD)
     //   128-wide blocks in E5M2: non-temporal, or through where the launch says so (y_keep, see there).  The output is the
     //     larger part of what moves, and the last-level cache keeps the inputs instead of it: 53248 x 16384, 1000 tokens, with
     //     the quantiser 95 / 93 / 78, cold 111 / 109 / 114; 2048 tokens, fp32 output 180 / 182 / 157, cold 183 / 183 / 171.
-    //   128-wide blocks with an epilogue of their own: non-temporal, Z too.  Rows of few blocks write more than they read, and the
+    //   128-wide blocks with an epilogue of their own: non-temporal, and so is Z beside a Y in bf16 (beside one in fp32 it leaves in
+    //     single values, ordinary).  Rows of few blocks write more than they read, and the
     //     L2 keeps the activations instead: 14336 x 4096 at 95 %, 4096 tokens, ordinary / non-temporal 57.6 / 44.2, with SiLU 63.6 /
     //     50.5, with Z 75.7 / 61.5; with the 4096 x 14336 product that reads it behind it 101.8 / 103.0, with Z 124.4 / 111.1; 4096
     //     and 14336 at 80 %, 2048 tokens, both products 133.6 / 131.2; 16384 and 53248 at 95 %, 1024 tokens 271.4 / 271.4.
     //   An output whose rows may not be stored in pairs: ordinary, so that the L2 puts lines together that are written in
     //     parts.  (Through or past it with rows two apart: up to 1.9 times as long; 8192 x 3072 at 70 %, 64-wide, 2048 tokens,
     //     odd pitch, fp32 47.0 / 61.5 us, in E5M2 with 14336 x 4096 at 90 %, 128-wide, bf16 29.3 / 56.0.)
+    //   A Y that may be, in an instance without pairs because of the residual or Z beside it: as other Y of its block.  It makes no
+    //     difference in bf16, whose lines then leave in halves (the policy of its block / ordinary: 14336 x 4096 at 90 %, 64-wide, 2048 tokens,
+    //     odd residual 60.3 / 60.1 us, odd Z 70.4 / 71.0; at 95 %, 128-wide, 4096 tokens 80.5 / 80.9, 103.6 / 103.6).
     enum { kStoreOrdinary, kStoreThrough, kStoreStreaming };
     constexpr int kStores = B < 128 ? kStoreThrough : F8 || EPI::kOn ? kStoreStreaming : kStoreOrdinary;
     if (a.y_fast && !(CHUNK && shared_row)) {
