@@ -602,6 +602,103 @@ int blast_norm_residual_backward(const blast_norm_view* P, const void* h_out, in
                                  void* stream);
 int blast_norm_residual_backward_workspace(const blast_norm_view* P, int64_t T, size_t* ws_bytes /* HOST */);
 
+/*
+ * ---- scaled 8-bit activations and weights -------------------------------------------------------------------------------------
+ *
+ * Codes in 8-bit floating point with a power of two for each token and group of 64 or 128 features: what a product reads, what the
+ * epilogue of another one writes, and the form in which a training step keeps activations for the way back.  Element (t, k) is
+ * codes[t*ld + k] * 2^(scales[(k/group)*lds + t] - 127); in a weight every stored block has one such scale.
+ *
+ * Every call that writes the form takes the smallest scale from 2^-100 on that brings the group's largest finite magnitude to at most
+ * the format's largest value, and rounds the quotient to nearest, ties to the even mantissa.  Zeros stay zeros, NaN stays NaN; an infinity is
+ * one in E5M2 and NaN in E4M3; a finite magnitude beyond 1.75 * 2^127 counts as that.  A group's scale is a byte from 27 to 246; other
+ * bytes in what a call reads are not checked.
+ */
+#define BLAST_E4M3 0 /* 4 exponent bits (bias 7), 3 of mantissa, no infinities, 0x7F / 0xFF NaN, largest value 448 */
+#define BLAST_E5M2 1 /* as in blast_quantize_e5m2, largest value 57344 */
+
+/* A plain view like blast_bsr_view: device memory, the struct is read at call time. */
+typedef struct blast_scaled8_view {
+  uint8_t* codes;  /* token-major [T][K] */
+  int64_t ld;      /* row pitch, bytes, >= K */
+  uint8_t* scales; /* [ceil(K / group)][lds], 16-byte aligned */
+  int64_t lds;     /* >= T, a multiple of 16 */
+  int32_t format;  /* BLAST_E4M3 or BLAST_E5M2 */
+  int32_t group;   /* 64 or 128 */
+} blast_scaled8_view;
+
+/* The values of a packed matrix in 8 bits; the structure stays that of its blast_bsr_view, whose vals are not read. */
+typedef struct blast_weight8_view {
+  const uint8_t* vals8;  /* [nnz][b][b] in the order of vals, 16-byte aligned */
+  const uint8_t* scales; /* [nnz], 16-byte aligned, readable up to the next multiple of 16 */
+  int32_t format;
+} blast_weight8_view;
+
+/*
+ * blast_quantize_scaled8: X (fp32 or bf16, token-major [T][K], row pitch ldx elements) into `out`; only codes of K features and scales of T
+ * tokens are written.  blast_dequantize_scaled8: back, exact in either type.  Any pitch and alignment of X, Y and the
+ * codes; 16-byte aligned rows of X, 8-byte aligned rows of codes and K a multiple of 8 are read and written in one piece a lane.
+ * blast_bsr_quantize_scaled8: the stored blocks of W (b = 64 or 128), one scale a block.
+ * Never synchronise.  Errors: INVALID_ARG, UNSUPPORTED_BLOCK, HIP.
+ */
+int blast_quantize_scaled8(const void* X, int64_t ldx, int32_t x_dtype, int64_t T, int64_t K, const blast_scaled8_view* out,
+                           void* stream);
+int blast_dequantize_scaled8(const blast_scaled8_view* X, int64_t T, int64_t K, void* Y, int64_t ldy, int32_t y_dtype, void* stream);
+int blast_bsr_quantize_scaled8(const blast_bsr_view* W, int32_t format, uint8_t* vals8 /* out, as in blast_weight8_view */,
+                               uint8_t* scales /* out */, void* stream);
+
+/*
+ * blast_bsr_linear on scaled 8-bit operands:  Z = W~ X + bias,  Y = act(Z) + R  (b = 64 or 128, token-major).
+ *   W, W8               structure (row_ptr, col_idx, row_order, nnz, b) and values
+ *   X                   scaled 8-bit [T][cols], group >= b, codes 16-byte aligned, ld % 16 == 0
+ *   bias, act, R        as in blast_bsr_linear (R fp32 or bf16 [T][rows])
+ *   Y, ldy, y_dtype     out, fp32 or bf16, may be NULL; may be R (same pitch and type)
+ *   Y8                  out, the same values in scaled 8-bit form, group = b, codes and pitch as X; may be NULL
+ *   Z8                  out, Z in scaled 8-bit form, likewise; may be NULL: what blast_act_backward_scaled8 reads
+ * Products are summed in fp32; bias, activation and residual are added in fp32, with one rounding when a value is stored.  Without an fp32 Y the products
+ * come from the 8-bit matrix instruction, which drops low bits of a product next to larger ones (root mean square error 1.5e-5 of a sum,
+ * 1/130 of bf16's half step); with one they are those of the exactly widened values, at the 16-bit instruction's rate.
+ * Rows are never cut into chunks: sums have a fixed order.  No output overlaps another or an input, R = Y apart.
+ * Never synchronises.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED_BLOCK, HIP.
+ */
+int blast_bsr_linear_scaled8(const blast_bsr_view* W, const blast_weight8_view* W8, const blast_scaled8_view* X, int64_t T,
+                             const float* bias, int32_t act, const void* R, int64_t ldr, int32_t r_dtype, void* Y, int64_t ldy,
+                             int32_t y_dtype, const blast_scaled8_view* Y8, const blast_scaled8_view* Z8, void* stream);
+
+/*
+ * The gated half of Eq. (1) in one launch:  G = Wgate X,  U = Wup X,  H = act(G) (.) U.
+ *   H, ldh              out, bf16 [T][rows], may be NULL
+ *   H8, G8, U8          out, scaled 8-bit, group = b, each may be NULL (not H and H8 both): what the next product, the gradients of the
+ *                       blocks and blast_act_backward_scaled8 read.  The activation takes G and U before they are rounded.
+ * act, operands, arithmetic (the 8-bit instruction's) and errors as in blast_bsr_linear_scaled8; BLAST_ACT_NONE is a product of the two.
+ */
+int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_weight8_view* gate8, const blast_bsr_view* Wup,
+                            const blast_weight8_view* up8, const blast_scaled8_view* X, int64_t T, int32_t act, uint16_t* H,
+                            int64_t ldh, const blast_scaled8_view* H8, const blast_scaled8_view* G8, const blast_scaled8_view* U8,
+                            void* stream);
+
+/*
+ * blast_bsr_sddmm with X as it was kept in scaled 8-bit form: dvals[q] = the entries of dY X^T on stored block q, the codes widened exactly
+ * to bf16, fp32 sums in a fixed order (b = 64 or 128).
+ *   dY, ldy             bf16 token-major [T][rows], 16-byte aligned, ldy % 8 == 0
+ *   X                   scaled 8-bit [T][cols], group >= b, codes 16-byte aligned, ld % 16 == 0
+ *   dvals               out, fp32 [nnz][b][b], 16-byte aligned; T = 0 gives zeros
+ *   ws, ws_bytes        blast_bsr_sddmm_scaled8_workspace() bytes, 16-byte aligned (sums over runs of tokens, where there are few blocks)
+ * Never synchronises.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED_BLOCK, WORKSPACE, HIP.
+ */
+int blast_bsr_sddmm_scaled8(const blast_bsr_view* W, const uint16_t* dY, int64_t ldy, const blast_scaled8_view* X, int64_t T,
+                            float* dvals, void* ws, size_t ws_bytes, void* stream);
+int blast_bsr_sddmm_scaled8_workspace(const blast_bsr_view* W, int64_t T, size_t* ws_bytes /* HOST */);
+
+/*
+ * blast_act_backward with Z (and U) as they were kept in scaled 8-bit form, [T][N] in groups of either size, any pitch and
+ * alignment of the codes.  Z is required; everything else as there, the workspace is blast_act_backward_workspace()'s.
+ */
+int blast_act_backward_scaled8(const blast_scaled8_view* Z, const blast_scaled8_view* U, const void* dY, int64_t lddy,
+                               int32_t dy_dtype, int64_t T, int64_t N, int32_t act, uint16_t* dZ, int64_t lddz, uint16_t* dU,
+                               int64_t lddu, uint16_t* H, int64_t ldh, float* dbias_z, float* dbias_u, void* ws, size_t ws_bytes,
+                               void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,7 @@ F32, BF16 = 0, 1
 ACT = {"silu": 0, "gelu": 1, "relu": 2}
 ACT_NONE = -1
 NORM = {"rms": 0, "layer": 1}
+FORMAT8 = {"e4m3": 0, "e5m2": 1}
 
 EXPORTS = (
     "blast_strerror", "blast_n_keep", "blast_bsr_aux_bytes", "blast_bsr_pack_bound", "blast_bsr_pack", "blast_bsr_pack_enqueue",
@@ -35,6 +36,8 @@ EXPORTS = (
     "blast_sparse_mlp_handover_test", "blast_sparse_mlp_e5m2w", "blast_sparse_mlp_e5m2w_workspace",
     "blast_bsr_linear", "blast_act_backward", "blast_act_backward_workspace", "blast_norm_residual",
     "blast_norm_residual_backward", "blast_norm_residual_backward_workspace",
+    "blast_quantize_scaled8", "blast_dequantize_scaled8", "blast_bsr_quantize_scaled8", "blast_bsr_linear_scaled8",
+    "blast_bsr_gated_scaled8", "blast_bsr_sddmm_scaled8", "blast_bsr_sddmm_scaled8_workspace", "blast_act_backward_scaled8",
 )
 
 
@@ -58,6 +61,17 @@ class NormView(C.Structure):
         ("p_dtype", C.c_int32), ("g_dtype", C.c_int32), ("weight", C.c_void_p), ("bias", C.c_void_p),
         ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("gate", C.c_void_p), ("ldg", C.c_int64),
     ]
+
+
+class Scaled8View(C.Structure):
+    _fields_ = [
+        ("codes", C.c_void_p), ("ld", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64), ("format", C.c_int32),
+        ("group", C.c_int32),
+    ]
+
+
+class Weight8View(C.Structure):
+    _fields_ = [("vals8", C.c_void_p), ("scales", C.c_void_p), ("format", C.c_int32)]
 
 
 _lib = None
@@ -155,6 +169,18 @@ def lib():
                                                    i64, i32, vp, i64, vp, vp, vp, vp, vp, sz, vp]
         L.blast_norm_residual_backward_workspace.restype = C.c_int
         L.blast_norm_residual_backward_workspace.argtypes = [pn, i64, C.POINTER(sz)]
+        pe, pw = C.POINTER(Scaled8View), C.POINTER(Weight8View)
+        for name, args in (
+                ("blast_quantize_scaled8", [vp, i64, i32, i64, i64, pe, vp]),
+                ("blast_dequantize_scaled8", [pe, i64, i64, vp, i64, i32, vp]),
+                ("blast_bsr_quantize_scaled8", [pv, i32, vp, vp, vp]),
+                ("blast_bsr_linear_scaled8", [pv, pw, pe, i64, vp, i32, vp, i64, i32, vp, i64, i32, pe, pe, vp]),
+                ("blast_bsr_gated_scaled8", [pv, pw, pv, pw, pe, i64, i32, vp, i64, pe, pe, pe, vp]),
+                ("blast_bsr_sddmm_scaled8", [pv, vp, i64, pe, i64, vp, vp, sz, vp]),
+                ("blast_bsr_sddmm_scaled8_workspace", [pv, i64, C.POINTER(sz)]),
+                ("blast_act_backward_scaled8", [pe, pe, vp, i64, i32, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = C.c_int, args
         _lib = L
     return _lib
 
@@ -864,3 +890,244 @@ def norm_residual_backward(h_out: torch.Tensor, y: Optional[torch.Tensor], stats
         _dtype_code(dx.dtype), dhop, lddho, T, dhp, lddh, dyp, lddy, _dtype_code(dy_dtype), _ptr(dgate), lddg, _ptr(dweight),
         _ptr(dbias), _ptr(dpost_weight), _ptr(dpost_bias), _ptr(ws), ws_bytes, _stream()), "blast_norm_residual_backward")
     return NormGrads(dh, dy, dgate, dweight, dbias, dpost_weight, dpost_bias)
+
+
+# ---- scaled 8-bit activations and weights -------------------------------------------------------------------------------
+
+@dataclass
+class Scaled8:
+    """A scaled 8-bit tensor (blast_scaled8_view): element (t, k) is codes[t, k] * 2^(scales[k // group, t] - 127)."""
+    codes: torch.Tensor  # uint8 [T, K], rows contiguous
+    scales: torch.Tensor  # uint8 [ceil(K / group), >= T, a multiple of 16], contiguous
+    group: int  # 64 or 128
+    fmt: str = "e4m3"  # or "e5m2"
+
+    def view(self, shape=None) -> Scaled8View:
+        """The C struct of this tensor, which is of that shape if one is given."""
+        codes, scales = self.codes, self.scales
+        assert codes.is_cuda and codes.dtype == torch.uint8 and codes.dim() == 2 and (shape is None or codes.shape == shape), (codes.shape, shape)
+        T, K = codes.shape
+        assert codes.stride(1) == 1 or K <= 1
+        assert scales.is_cuda and scales.dtype == torch.uint8 and scales.dim() == 2 and scales.is_contiguous()
+        assert scales.shape[0] == -(-K // self.group) and scales.shape[1] >= T
+        ld = codes.stride(0)
+        return Scaled8View(codes.data_ptr(), ld if T > 1 or ld > K else -(-K // 16) * 16, scales.data_ptr(), scales.shape[1],
+                           FORMAT8[self.fmt], self.group)
+
+
+@dataclass
+class Weight8:
+    """A packed matrix with its stored blocks in 8 bits, one scale each."""
+    packed: PackedBsr
+    codes: torch.Tensor  # uint8 [nnz, b, b]
+    scales: torch.Tensor  # uint8 [nnz], readable to the next multiple of 16
+    fmt: str = "e4m3"
+
+    def view(self) -> Weight8View:
+        p = self.packed
+        assert self.codes.is_cuda and self.codes.dtype == torch.uint8 and self.codes.is_contiguous()
+        assert self.codes.numel() >= p.nnz * p.b * p.b and self.scales.dtype == torch.uint8 and self.scales.numel() >= p.nnz
+        return Weight8View(self.codes.data_ptr(), self.scales.data_ptr(), FORMAT8[self.fmt])
+
+
+def empty_scaled8(T: int, K: int, *, group: int = 128, fmt: str = "e4m3", device="cuda") -> Scaled8:
+    """An uninitialised scaled 8-bit tensor of T tokens and K features."""
+    lds = -(-T // 16) * 16
+    codes = torch.empty((T, -(-K // 16) * 16), dtype=torch.uint8, device=device)
+    return Scaled8(codes if codes.shape[1] == K else codes[:, :K],
+                   torch.empty((-(-K // group), lds), dtype=torch.uint8, device=device), group, fmt)
+
+
+def _quantize_args(x: torch.Tensor, out: Scaled8):
+    assert x.dim() == 2
+    v = out.view(x.shape)
+    return (*_rows_of(x, x.shape, _EITHER), _dtype_code(x.dtype), *x.shape, v)
+
+
+def quantize_scaled8(x: torch.Tensor, *, group: int = 128, fmt: str = "e4m3", out: Optional[Scaled8] = None) -> Scaled8:
+    """blast_quantize_scaled8: fp32 or bf16 [T, K] to codes with a scale for each token and group of features."""
+    q = out if out is not None else empty_scaled8(*x.shape, group=group, fmt=fmt, device=x.device)
+    _check(lib().blast_quantize_scaled8(*_quantize_args(x, q), _stream()), "blast_quantize_scaled8")
+    return q
+
+
+def prepare_quantize_scaled8(x: torch.Tensor, out: Scaled8) -> PreparedCall:
+    """blast_quantize_scaled8 on the current stream with fixed buffers, as a PreparedCall."""
+    L = lib()
+    *args, v = _quantize_args(x, out)
+    types = L.blast_quantize_scaled8.argtypes
+    args = [t(a) for t, a in zip(types, args)] + [C.byref(v), C.c_void_p(_stream())]
+    return PreparedCall(L.blast_quantize_scaled8, "blast_quantize_scaled8", tuple(args), (v, x, out))
+
+
+def dequantize_scaled8(q: Scaled8, *, out_dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """blast_dequantize_scaled8: the values, bf16 or fp32 [T, K]."""
+    T, K = q.codes.shape
+    y = out if out is not None else torch.empty((T, K), dtype=out_dtype, device=q.codes.device)
+    p, ld = _rows_of(y, (T, K), _EITHER)
+    _check(lib().blast_dequantize_scaled8(q.view(), T, K, p, ld, _dtype_code(y.dtype), _stream()), "blast_dequantize_scaled8")
+    return y
+
+
+def bsr_quantize_scaled8(W: PackedBsr, *, fmt: str = "e4m3") -> Weight8:
+    """blast_bsr_quantize_scaled8: the stored blocks in 8 bits, one scale a block (64- or 128-wide blocks)."""
+    dev, n = W.vals.device, W.nnz
+    codes = torch.empty((n, W.b, W.b), dtype=torch.uint8, device=dev)
+    scales = torch.empty(max(-(-n // 16) * 16, 16), dtype=torch.uint8, device=dev)
+    v = W.view()
+    _check(lib().blast_bsr_quantize_scaled8(C.byref(v), FORMAT8[fmt], codes.data_ptr(), scales.data_ptr(), _stream()),
+           "blast_bsr_quantize_scaled8")
+    return Weight8(W, codes, scales[:n], fmt)
+
+
+def _out8(q: Optional[Scaled8], shape) -> Optional[Scaled8View]:
+    return None if q is None else q.view(shape)
+
+
+def _ref(v):
+    return None if v is None else C.byref(v)
+
+
+def _linear8_args(W: Weight8, X: Scaled8, out, bias, act, residual, pre):
+    """Arguments without the stream, and the structs that they point to."""
+    p = W.packed
+    T, K = X.codes.shape
+    assert K == p.cols
+    shape = (T, p.rows)
+    y, ldy, y8, y_dtype = None, 0, None, F32
+    if isinstance(out, Scaled8):
+        y8 = out.view(shape)
+    else:
+        y, ldy = _rows_of(out, shape, _EITHER)
+        y_dtype = _dtype_code(out.dtype)
+    r, ldr = _rows_of(residual, shape, _EITHER)
+    v, w, x, z8 = p.view(), W.view(), X.view(), _out8(pre, shape)
+    return (C.byref(v), C.byref(w), C.byref(x), T, _vector(bias, p.rows, (torch.float32,)), ACT_NONE if act is None else ACT[act], r,
+            ldr, F32 if r is None else _dtype_code(residual.dtype), y, ldy, y_dtype, _ref(y8), _ref(z8)), (v, w, x, y8, z8)
+
+
+def bsr_linear_scaled8(W: Weight8, X: Scaled8, *, bias: Optional[torch.Tensor] = None, act: Optional[str] = None,
+                       residual: Optional[torch.Tensor] = None, pre: Optional[Scaled8] = None, out_dtype: torch.dtype = torch.float32,
+                       out_fmt: Optional[str] = None, out=None):
+    """blast_bsr_linear_scaled8: Y = act(W X + bias) + residual as fp32 or bf16 (out_dtype), or with out_fmt ("e4m3", "e5m2") as a Scaled8 in
+    groups of a block's rows; `out` is either.  pre: a Scaled8 that receives W X + bias, what act_backward_scaled8 reads."""
+    T, rows, dev = X.codes.shape[0], W.packed.rows, X.codes.device
+    if out is None:
+        out = torch.empty((T, rows), dtype=out_dtype, device=dev) if out_fmt is None else \
+            empty_scaled8(T, rows, group=W.packed.b, fmt=out_fmt, device=dev)
+    args, _ = _linear8_args(W, X, out, bias, act, residual, pre)
+    _check(lib().blast_bsr_linear_scaled8(*args, _stream()), "blast_bsr_linear_scaled8")
+    return out
+
+
+def _prepared(fn, where, args, keep) -> PreparedCall:
+    """Numbers as the C types that the function declares; pointers to structs as they are."""
+    types = fn.argtypes
+    return PreparedCall(fn, where, tuple(a if a is None or not isinstance(a, (int, float)) else t(a) for t, a in zip(types, args)), keep)
+
+
+def prepare_bsr_linear_scaled8(W: Weight8, X: Scaled8, out, *, bias: Optional[torch.Tensor] = None, act: Optional[str] = None,
+                               residual: Optional[torch.Tensor] = None, pre: Optional[Scaled8] = None) -> PreparedCall:
+    """blast_bsr_linear_scaled8 on the current stream with fixed buffers, as a PreparedCall."""
+    L = lib()
+    args, views = _linear8_args(W, X, out, bias, act, residual, pre)
+    return _prepared(L.blast_bsr_linear_scaled8, "blast_bsr_linear_scaled8", args + (_stream(),), (views, W, X, out, bias, residual, pre))
+
+
+@dataclass
+class Gated8:
+    """H = act(G) * U of bsr_gated_scaled8, and G and U where they were kept."""
+    H: object  # Scaled8 or bf16 [T, rows]
+    G: Optional[Scaled8] = None
+    U: Optional[Scaled8] = None
+
+
+def _gated8_args(gate: Weight8, up: Weight8, X: Scaled8, out, act, keep):
+    p, q = gate.packed, up.packed
+    T, K = X.codes.shape
+    assert K == p.cols and (p.rows, p.cols, p.b) == (q.rows, q.cols, q.b)
+    shape = (T, p.rows)
+    h, ldh, h8 = None, 0, None
+    if isinstance(out, Scaled8):
+        h8 = out.view(shape)
+    else:
+        h, ldh = _rows_of(out, shape, (torch.bfloat16,))
+    vg, wg, vu, wu, x = p.view(), gate.view(), q.view(), up.view(), X.view()
+    g8, u8 = (None, None) if keep is None else (keep[0].view(shape), keep[1].view(shape))
+    return (C.byref(vg), C.byref(wg), C.byref(vu), C.byref(wu), C.byref(x), T, ACT_NONE if act is None else ACT[act], h, ldh, _ref(h8),
+            _ref(g8), _ref(u8)), (vg, wg, vu, wu, x, h8, g8, u8)
+
+
+def bsr_gated_scaled8(gate: Weight8, up: Weight8, X: Scaled8, *, act: Optional[str] = "silu", keep: bool = False,
+                      out_fmt: Optional[str] = "e4m3", out=None) -> Gated8:
+    """blast_bsr_gated_scaled8: H = act(Wgate X) * (Wup X) as a Scaled8 in groups of a block's rows (out_fmt None: bf16); with `keep` the
+    two products in E4M3 too, what gated_act_backward_scaled8 reads."""
+    T, rows, b, dev = X.codes.shape[0], gate.packed.rows, gate.packed.b, X.codes.device
+    if out is None:
+        out = torch.empty((T, rows), dtype=torch.bfloat16, device=dev) if out_fmt is None else \
+            empty_scaled8(T, rows, group=b, fmt=out_fmt, device=dev)
+    kept = tuple(empty_scaled8(T, rows, group=b, device=dev) for _ in range(2)) if keep else None
+    args, _ = _gated8_args(gate, up, X, out, act, kept)
+    _check(lib().blast_bsr_gated_scaled8(*args, _stream()), "blast_bsr_gated_scaled8")
+    return Gated8(out, *(kept or ()))
+
+
+def prepare_bsr_gated_scaled8(gate: Weight8, up: Weight8, X: Scaled8, out, *, act: Optional[str] = "silu", keep=None) -> PreparedCall:
+    """blast_bsr_gated_scaled8 on the current stream with fixed buffers, as a PreparedCall.  keep: two Scaled8 for G and U."""
+    L = lib()
+    args, views = _gated8_args(gate, up, X, out, act, keep)
+    return _prepared(L.blast_bsr_gated_scaled8, "blast_bsr_gated_scaled8", args + (_stream(),), (views, gate, up, X, out, keep))
+
+
+def bsr_sddmm_scaled8(W: PackedBsr, dY: torch.Tensor, X: Scaled8, *, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """blast_bsr_sddmm_scaled8: gradient of the stored blocks, fp32 [nnz, b, b], from dY in bf16 and X as it was kept."""
+    L = lib()
+    T, K = X.codes.shape
+    assert K == W.cols
+    dy, ldy = _rows_of(dY, (T, W.rows), (torch.bfloat16,))
+    dv = out if out is not None else torch.empty((W.nnz, W.b, W.b), dtype=torch.float32, device=dY.device)
+    assert dv.is_cuda and dv.dtype == torch.float32 and dv.is_contiguous() and dv.numel() == W.nnz * W.b * W.b
+    v, wsb = W.view(), C.c_size_t(0)
+    _check(L.blast_bsr_sddmm_scaled8_workspace(C.byref(v), T, C.byref(wsb)), "blast_bsr_sddmm_scaled8_workspace")
+    ws = torch.empty(wsb.value, dtype=torch.uint8, device=dY.device) if wsb.value else None
+    _check(L.blast_bsr_sddmm_scaled8(C.byref(v), dy, ldy, X.view(), T, dv.data_ptr(), _ptr(ws), wsb.value, _stream()),
+           "blast_bsr_sddmm_scaled8")
+    return dv
+
+
+def _act_backward8(Z, U, dY, act, dZ, dU, H, dbias_z, dbias_u):
+    assert dY.dim() == 2
+    L, shape, low = lib(), dY.shape, (torch.bfloat16,)
+    T, N = shape
+    wanted, ws, ws_bytes = (dbias_z is not None) + (dbias_u is not None), None, 0
+    if wanted:
+        wsb = C.c_size_t(0)
+        _check(L.blast_act_backward_workspace(T, N, wanted, C.byref(wsb)), "blast_act_backward_workspace")
+        ws_bytes = wsb.value
+        ws = dY.new_empty(ws_bytes, dtype=torch.uint8) if ws_bytes else None
+    _check(L.blast_act_backward_scaled8(Z.view(shape), None if U is None else U.view(shape), *_rows_of(dY, shape, _EITHER),
+                                        _dtype_code(dY.dtype), T, N, ACT_NONE if act is None else ACT[act], *_rows_of(dZ, shape, low),
+                                        *_rows_of(dU, shape, low), *_rows_of(H, shape, low), _ptr(dbias_z), _ptr(dbias_u), _ptr(ws),
+                                        ws_bytes, _stream()), "blast_act_backward_scaled8")
+
+
+def act_backward_scaled8(Z: Scaled8, dY: torch.Tensor, *, act: Optional[str] = None, bias_grad: bool = False,
+                         out: Optional[torch.Tensor] = None) -> ActGrads:
+    """act_backward with Z as it was kept in 8 bits (the `pre` of bsr_linear_scaled8)."""
+    dZ = out if out is not None else torch.empty_like(dY, dtype=torch.bfloat16)
+    db = dY.new_empty(dY.shape[1], dtype=torch.float32) if bias_grad else None
+    _act_backward8(Z, None, dY, act, dZ, None, None, db, None)
+    return ActGrads(dZ=dZ, dbias=db)
+
+
+def gated_act_backward_scaled8(G: Scaled8, U: Scaled8, dH: torch.Tensor, *, act: str = "silu", bias_grad: bool = False,
+                               with_h: bool = True) -> ActGrads:
+    """gated_act_backward with G and U as they were kept in 8 bits."""
+    assert U is not None
+    dG, dU = torch.empty_like(dH, dtype=torch.bfloat16), torch.empty_like(dH, dtype=torch.bfloat16)
+    H = torch.empty_like(dH, dtype=torch.bfloat16) if with_h else None
+    dbg = dbu = None
+    if bias_grad:
+        dbg, dbu = dH.new_empty(dH.shape[1], dtype=torch.float32), dH.new_empty(dH.shape[1], dtype=torch.float32)
+    _act_backward8(G, U, dH, act, dG, dU, H, dbg, dbu)
+    return ActGrads(None, None, dG, dU, H, dbg, dbu)

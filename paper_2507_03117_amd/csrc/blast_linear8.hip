@@ -1,0 +1,130 @@
+// Products of scaled 8-bit operands (kern_linear8.h).
+#include "scaled8_check.h"
+
+#include "kern_linear8.h"
+
+using namespace blast_dev;
+
+namespace {
+
+int check_weight(const blast_bsr_view* W, const blast_weight8_view* W8) {
+  if (!W || !W->row_ptr || !W8 || !format8_ok(W8->format)) return BLAST_ERR_INVALID_ARG;
+  if (W->rows < 0 || W->cols < 0 || W->nnz < 0 || W->nnz > INT32_MAX) return BLAST_ERR_INVALID_ARG;
+  if (W->b != 64 && W->b != 128) return BLAST_ERR_UNSUPPORTED_BLOCK;
+  if (W->rows % W->b || W->cols % W->b) return BLAST_ERR_SHAPE;
+  if (W->rows > INT32_MAX / 2 || W->cols > INT32_MAX / 2) return BLAST_ERR_INVALID_ARG;
+  if (W->nnz > 0 && (!W->col_idx || !W8->vals8 || !blast::aligned(W8->vals8, 16) || !W8->scales || !blast::aligned(W8->scales, 16)))
+    return BLAST_ERR_INVALID_ARG;
+  return BLAST_OK;
+}
+
+Mat8 mat8_of(const blast_bsr_view* W, const blast_weight8_view* W8) { return Mat8{W->row_ptr, W->col_idx, W8->vals8, W8->scales}; }
+
+// An output in scaled 8-bit form: in groups of a block's rows.
+int check_out8(const blast_scaled8_view* v, const blast_bsr_view* W, int64_t T) {
+  if (!v) return BLAST_OK;
+  if (v->group != W->b) return BLAST_ERR_INVALID_ARG;
+  return check_eight(v, T, W->rows, 16);
+}
+
+template <int B, int TT, bool DUAL, bool EXACT>
+int launch_linear8(Linear8Args a, hipStream_t stream) {
+  using C = L8Cfg<B, TT, DUAL>;
+  static blast::DeviceFlags lds_set;
+  int dev = 0;
+  BLAST_HIP_TRY(hipGetDevice(&dev));
+  if (!lds_set.test(dev)) {
+    BLAST_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_linear8<B, TT, DUAL, EXACT>),
+                                      hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES));
+    lds_set.set(dev);
+  }
+  a.ntt = (int)(((int64_t)a.T + TT - 1) / TT);
+  const int64_t grid = ((int64_t)a.nbr + 7) / 8 * 8 * a.ntt;
+  if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
+  k_linear8<B, TT, DUAL, EXACT><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a);
+  BLAST_LAUNCH_CHECK("k_linear8");
+  return BLAST_OK;
+}
+
+}  // namespace
+
+extern "C" int blast_bsr_linear_scaled8(const blast_bsr_view* W, const blast_weight8_view* W8, const blast_scaled8_view* X, int64_t T,
+                                        const float* bias, int32_t act, const void* R, int64_t ldr, int32_t r_dtype, void* Y,
+                                        int64_t ldy, int32_t y_dtype, const blast_scaled8_view* Y8, const blast_scaled8_view* Z8,
+                                        void* stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (int rc = check_weight(W, W8)) return rc;
+  if (T < 0 || T > INT32_MAX / 2) return BLAST_ERR_INVALID_ARG;
+  if (act < BLAST_ACT_NONE || act > BLAST_ACT_RELU) return BLAST_ERR_INVALID_ARG;
+  if (Y && y_dtype != BLAST_F32 && y_dtype != BLAST_BF16) return BLAST_ERR_INVALID_ARG;
+  if (R && r_dtype != BLAST_F32 && r_dtype != BLAST_BF16) return BLAST_ERR_INVALID_ARG;
+  if (int rc = check_eight(X, T, W->cols, 16)) return rc;
+  if (X->group < W->b) return BLAST_ERR_INVALID_ARG;
+  if (int rc = check_out8(Y8, W, T)) return rc;
+  if (int rc = check_out8(Z8, W, T)) return rc;
+  if (T == 0 || W->rows == 0) return BLAST_OK;
+  if (!Y && !Y8) return BLAST_ERR_INVALID_ARG;
+  if ((Y && ldy < W->rows) || (R && ldr < W->rows)) return BLAST_ERR_INVALID_ARG;
+  if (W->cols == 0 && W->nnz > 0) return BLAST_ERR_SHAPE;
+  Linear8Args a{};
+  a.m[0] = mat8_of(W, W8);
+  a.row_order = W->row_order;
+  a.x = eight_of(X);
+  a.wfmt = W8->format;
+  a.T = (int)T;
+  a.nbr = (int)(W->rows / W->b);
+  a.act = act;
+  a.bias = bias;
+  a.r = R;
+  a.ldr = ldr;
+  a.r_bf16 = r_dtype == BLAST_BF16;
+  a.y = Y;
+  a.ldy = ldy;
+  a.y_bf16 = y_dtype == BLAST_BF16;
+  a.r_vec = blast::aligned(R, 16) && ldr * (a.r_bf16 ? 2 : 4) % 16 == 0;
+  a.y_vec = blast::aligned(Y, 16) && ldy * (a.y_bf16 ? 2 : 4) % 16 == 0;
+  if (Y8) a.y8 = eight_of(Y8);
+  if (Z8) a.k8[0] = eight_of(Z8);
+  const bool exact = Y && !a.y_bf16;
+  if (W->b == 64) return exact ? launch_linear8<64, 128, false, true>(a, stream) : launch_linear8<64, 128, false, false>(a, stream);
+  return exact ? launch_linear8<128, 128, false, true>(a, stream) : launch_linear8<128, 128, false, false>(a, stream);
+}
+
+extern "C" int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_weight8_view* gate8, const blast_bsr_view* Wup,
+                                       const blast_weight8_view* up8, const blast_scaled8_view* X, int64_t T, int32_t act, uint16_t* H,
+                                       int64_t ldh, const blast_scaled8_view* H8, const blast_scaled8_view* G8,
+                                       const blast_scaled8_view* U8, void* stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (int rc = check_weight(Wgate, gate8)) return rc;
+  if (int rc = check_weight(Wup, up8)) return rc;
+  if (Wgate->rows != Wup->rows || Wgate->cols != Wup->cols || Wgate->b != Wup->b) return BLAST_ERR_SHAPE;
+  if (gate8->format != up8->format) return BLAST_ERR_INVALID_ARG;
+  if (T < 0 || T > INT32_MAX / 2) return BLAST_ERR_INVALID_ARG;
+  if (act < BLAST_ACT_NONE || act > BLAST_ACT_RELU) return BLAST_ERR_INVALID_ARG;
+  if (int rc = check_eight(X, T, Wgate->cols, 16)) return rc;
+  if (X->group < Wgate->b) return BLAST_ERR_INVALID_ARG;
+  const blast_scaled8_view* outs[] = {H8, G8, U8};
+  for (const blast_scaled8_view* o : outs)
+    if (int rc = check_out8(o, Wgate, T)) return rc;
+  if (T == 0 || Wgate->rows == 0) return BLAST_OK;
+  if ((H != nullptr) == (H8 != nullptr)) return BLAST_ERR_INVALID_ARG;
+  if (H && ldh < Wgate->rows) return BLAST_ERR_INVALID_ARG;
+  if (Wgate->cols == 0 && (Wgate->nnz > 0 || Wup->nnz > 0)) return BLAST_ERR_SHAPE;
+  Linear8Args a{};
+  a.m[0] = mat8_of(Wgate, gate8);
+  a.m[1] = mat8_of(Wup, up8);
+  a.row_order = Wgate->row_order;
+  a.x = eight_of(X);
+  a.wfmt = gate8->format;
+  a.T = (int)T;
+  a.nbr = (int)(Wgate->rows / Wgate->b);
+  a.act = act;
+  a.y = H;
+  a.ldy = ldh;
+  a.y_bf16 = 1;
+  a.y_vec = blast::aligned(H, 16) && ldh * 2 % 16 == 0;
+  if (H8) a.y8 = eight_of(H8);
+  if (G8) a.k8[0] = eight_of(G8);
+  if (U8) a.k8[1] = eight_of(U8);
+  return Wgate->b == 64 ? launch_linear8<64, 128, true, false>(a, stream) : launch_linear8<128, 128, true, false>(a, stream);
+}

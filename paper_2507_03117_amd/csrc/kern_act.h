@@ -6,8 +6,10 @@
 // registers over the run and meet in LDS at its end, those of the runs in a second launch - or, for few rows, a workgroup has its
 // columns' rows to the end (k_act_backward_columns).  Measured: gated, 4096 x 14336, fp32 gradient 163 us (5.05 TB/s, the rate of a
 // large copy); GELU with the bias' gradient, 333 x 6400 7.4 us, 4096 x 6400 39 us.
+// EIGHT: Z and U in scaled 8-bit form (blast_act_backward_scaled8), a byte a value and a scale for a lane's eight.
 #pragma once
 #include "kern_rows.h"
+#include "kern_scaled8.h"
 
 namespace blast_dev {
 
@@ -20,6 +22,7 @@ struct ActArgs {
   int T, N, run;       // run: rows of a workgroup
   int tiles;           // column tiles
   int dy_bf16, act;
+  Eight z8, u8;        // in the place of z and u
 };
 
 // act(z) and act'(z)
@@ -48,19 +51,68 @@ __device__ __forceinline__ void act_and_slope(int act, float z, float& a, float&
 struct ActRow {
   Piece z, u, dy;
 };
-template <int NL, bool GATED, bool VEC>
+// A lane's eight values of a scaled 8-bit row: their codes in two words and their scale; element-wise a code and its scale a word.
+template <int NL, bool VEC>
+__device__ __forceinline__ void eight_load(Piece& q, const Eight& x, int t, int col0, int lane, int width) {
+  const uint8_t* row = x.codes + t * x.ld + col0;
+  const uint8_t* scales = x.scales + t;
+  if constexpr (VEC) {
+    const int e = lane * 8;
+    if (e < width) {
+      const u32x2v w = *reinterpret_cast<const u32x2v*>(row + e);
+      q.lo[0] = w[0];
+      q.lo[1] = w[1];
+      q.hi[0] = scales[(int64_t)((col0 + e) >> x.shift) * x.lds];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int e = piece_at<NL, false>(0, j, lane);
+      uint32_t v = 0;
+      if (e < width) v = row[e] | (uint32_t)scales[(int64_t)((col0 + e) >> x.shift) * x.lds] << 8;
+      if (j < 4)
+        q.lo[j & 3] = v;
+      else
+        q.hi[j & 3] = v;
+    }
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void eight_values(const Piece& q, int fmt, float (&out)[8]) {
+  if constexpr (VEC) {
+    decode8(u32x2v{q.lo[0], q.lo[1]}, fmt, scale_value((int)q.hi[0]), out);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t w = j < 4 ? q.lo[j & 3] : q.hi[j & 3];
+      out[j] = decode1((uint8_t)w, fmt, scale_value((int)(w >> 8)));
+    }
+  }
+}
+
+template <int NL, bool GATED, bool VEC, bool EIGHT>
 __device__ __forceinline__ void act_read(const ActArgs& a, ActRow& q, int t, int col0, int lane, int width) {
   q = ActRow{};
-  if (a.z) piece_load<NL, VEC>(q.z, row_of(a.z, t * a.ldz + col0, 1), 0, lane, width, 1);
-  if (GATED) piece_load<NL, VEC>(q.u, row_of(a.u, t * a.ldu + col0, 1), 0, lane, width, 1);
+  if constexpr (EIGHT) {
+    eight_load<NL, VEC>(q.z, a.z8, t, col0, lane, width);
+    if (GATED) eight_load<NL, VEC>(q.u, a.u8, t, col0, lane, width);
+  } else {
+    if (a.z) piece_load<NL, VEC>(q.z, row_of(a.z, t * a.ldz + col0, 1), 0, lane, width, 1);
+    if (GATED) piece_load<NL, VEC>(q.u, row_of(a.u, t * a.ldu + col0, 1), 0, lane, width, 1);
+  }
   piece_load<NL, VEC>(q.dy, row_of(a.dy, t * a.lddy + col0, a.dy_bf16), 0, lane, width, a.dy_bf16);
 }
-template <int NL, bool GATED, bool SUMS, bool VEC>
+template <int NL, bool GATED, bool SUMS, bool VEC, bool EIGHT>
 __device__ __forceinline__ void act_write(const ActArgs& a, const ActRow& q, int t, int col0, int lane, int width, float (&sum)[2][8]) {
   float zv[8], uv[8], d[8], av[8], dz[8], du[8];
-  piece_values<VEC>(q.z, 1, zv);
+  if constexpr (EIGHT) {
+    eight_values<VEC>(q.z, a.z8.fmt, zv);
+    if (GATED) eight_values<VEC>(q.u, a.u8.fmt, uv);
+  } else {
+    piece_values<VEC>(q.z, 1, zv);
+    if (GATED) piece_values<VEC>(q.u, 1, uv);
+  }
   piece_values<VEC>(q.dy, a.dy_bf16, d);
-  if (GATED) piece_values<VEC>(q.u, 1, uv);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     float slope;
@@ -82,7 +134,7 @@ __device__ __forceinline__ void act_write(const ActArgs& a, const ActRow& q, int
 
 constexpr int kActCols = 256, kActTeams = 8;
 
-template <bool GATED, bool SUMS, bool VEC>
+template <bool GATED, bool SUMS, bool VEC, bool EIGHT = false>
 __global__ __launch_bounds__(256) void k_act_backward(const ActArgs a) {
   const int lane = threadIdx.x & 31, team = threadIdx.x >> 5;
   const int tile = (int)blockIdx.x % a.tiles, run = (int)blockIdx.x / a.tiles;
@@ -93,8 +145,8 @@ __global__ __launch_bounds__(256) void k_act_backward(const ActArgs a) {
   for (int j = 0; j < 8; ++j) sum[0][j] = sum[1][j] = 0.0f;
   for (int t = run * a.run + team; t < t_end; t += kActTeams) {
     ActRow q;
-    act_read<32, GATED, VEC>(a, q, t, col0, lane, width);
-    act_write<32, GATED, SUMS, VEC>(a, q, t, col0, lane, width, sum);
+    act_read<32, GATED, VEC, EIGHT>(a, q, t, col0, lane, width);
+    act_write<32, GATED, SUMS, VEC, EIGHT>(a, q, t, col0, lane, width, sum);
   }
   if constexpr (SUMS) {
     __shared__ float red[kActTeams][kActCols];
@@ -124,7 +176,7 @@ __global__ __launch_bounds__(256) void k_act_backward(const ActArgs a) {
 // their way at a time, and nothing is left to be joined afterwards.  Two neighbouring workgroups of an XCD (ids eight apart)
 // share the 128-byte lines of bf16.
 constexpr int kActOwned = 32;
-template <bool GATED, bool VEC, int THREADS>
+template <bool GATED, bool VEC, int THREADS, bool EIGHT = false>
 __global__ __launch_bounds__(THREADS) void k_act_backward_columns(const ActArgs a) {
   constexpr int kLanes = kActOwned / 8, kRows = THREADS / kLanes, kWaves = THREADS / 64;
   const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes, id = blockIdx.x;
@@ -136,11 +188,11 @@ __global__ __launch_bounds__(THREADS) void k_act_backward_columns(const ActArgs 
   for (int j = 0; j < 8; ++j) sum[0][j] = sum[1][j] = 0.0f;
   for (int t = team; t < a.T; t += 2 * kRows) {
     ActRow q0, q1;
-    act_read<kLanes, GATED, VEC>(a, q0, t, col0, lane, width);
+    act_read<kLanes, GATED, VEC, EIGHT>(a, q0, t, col0, lane, width);
     const bool two = t + kRows < a.T;
-    if (two) act_read<kLanes, GATED, VEC>(a, q1, t + kRows, col0, lane, width);
-    act_write<kLanes, GATED, true, VEC>(a, q0, t, col0, lane, width, sum);
-    if (two) act_write<kLanes, GATED, true, VEC>(a, q1, t + kRows, col0, lane, width, sum);
+    if (two) act_read<kLanes, GATED, VEC, EIGHT>(a, q1, t + kRows, col0, lane, width);
+    act_write<kLanes, GATED, true, VEC, EIGHT>(a, q0, t, col0, lane, width, sum);
+    if (two) act_write<kLanes, GATED, true, VEC, EIGHT>(a, q1, t + kRows, col0, lane, width, sum);
   }
   // the sixteen rows of a wave, then the waves in order
   __shared__ float red[kWaves][kActOwned];
