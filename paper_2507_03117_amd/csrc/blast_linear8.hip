@@ -3,9 +3,13 @@
 
 #include "kern_linear8.h"
 
+
 using namespace blast_dev;
 
 namespace {
+
+// Fewer 128-token tiles than this are cut into tiles of 32 whose blocks eight waves share.
+constexpr int64_t kFewTiles = 384;
 
 int check_weight(const blast_bsr_view* W, const blast_weight8_view* W8) {
   if (!W || !W->row_ptr || !W8 || !format8_ok(W8->format)) return BLAST_ERR_INVALID_ARG;
@@ -27,23 +31,56 @@ int check_out8(const blast_scaled8_view* v, const blast_bsr_view* W, int64_t T) 
   return check_eight(v, T, W->rows, 16);
 }
 
-template <int B, int TT, bool DUAL, bool EXACT>
-int launch_linear8(Linear8Args a, hipStream_t stream) {
-  using C = L8Cfg<B, TT, DUAL>;
-  static blast::DeviceFlags lds_set;
+// Workgroups for tiles of TT tokens.  Many tiles: two XCDs share a block row, each with half of its tokens (53248 x 16384 at 95 %, 2048
+// tokens, one / two / four / eight XCDs to a row: 148 / 142 / 149 / 154 us; gated 14336 x 4096, 4096 tokens 85 / 84 / 85 / 84).  An odd
+// number of tiles leaves one of two XCDs a tile short.
+int64_t grid8(Linear8Args& a, int TT) {
+  a.ntt = (int)(((int64_t)a.T + TT - 1) / TT);
+  a.parts = TT >= 128 && a.ntt >= 2 && (a.ntt % 2 == 0 || a.ntt >= 16) ? 2 : 1;
+  const int64_t rows = 8 / a.parts;
+  return 8 * (((int64_t)a.nbr + rows - 1) / rows) * (((int64_t)a.ntt + a.parts - 1) / a.parts);
+}
+
+template <class K>
+int raise_lds(K kernel, int bytes, blast::DeviceFlags& set) {
   int dev = 0;
   BLAST_HIP_TRY(hipGetDevice(&dev));
-  if (!lds_set.test(dev)) {
-    BLAST_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_linear8<B, TT, DUAL, EXACT>),
-                                      hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES));
-    lds_set.set(dev);
+  if (!set.test(dev)) {
+    BLAST_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    set.set(dev);
   }
-  a.ntt = (int)(((int64_t)a.T + TT - 1) / TT);
-  const int64_t grid = ((int64_t)a.nbr + 7) / 8 * 8 * a.ntt;
+  return BLAST_OK;
+}
+
+template <int B, bool DUAL, bool EXACT, int WF, int XF>
+int launch_linear8(Linear8Args a, hipStream_t stream) {
+  const int64_t tiles = (int64_t)a.nbr * (((int64_t)a.T + 127) / 128);
+  static blast::DeviceFlags split_set, tile_set;
+  if (a.T <= 32 || tiles < kFewTiles) {
+    using C = S8Cfg<B, DUAL>;
+    if (int rc = raise_lds(&k_linear8_split<B, DUAL, EXACT, WF, XF>, C::LDS_BYTES, split_set)) return rc;
+    const int64_t grid = grid8(a, C::TT);
+    if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
+    k_linear8_split<B, DUAL, EXACT, WF, XF><<<dim3((unsigned)grid), dim3(64 * C::NW), C::LDS_BYTES, stream>>>(a);
+    BLAST_LAUNCH_CHECK("k_linear8_split");
+    return BLAST_OK;
+  }
+  using C = L8Cfg<B>;
+  if (int rc = raise_lds(&k_linear8<B, DUAL, EXACT, WF, XF>, C::LDS_BYTES, tile_set)) return rc;
+  const int64_t grid = grid8(a, C::TT);
   if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
-  k_linear8<B, TT, DUAL, EXACT><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a);
+  k_linear8<B, DUAL, EXACT, WF, XF><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a);
   BLAST_LAUNCH_CHECK("k_linear8");
   return BLAST_OK;
+}
+
+template <int B, bool DUAL>
+int by_formats(const Linear8Args& a, bool exact, hipStream_t stream) {
+  if constexpr (!DUAL)
+    if (exact) return launch_linear8<B, DUAL, true, 0, 0>(a, stream);
+  if (a.wfmt == BLAST_E4M3)
+    return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, false, 0, 0>(a, stream) : launch_linear8<B, DUAL, false, 0, 1>(a, stream);
+  return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, false, 1, 0>(a, stream) : launch_linear8<B, DUAL, false, 1, 1>(a, stream);
 }
 
 }  // namespace
@@ -86,8 +123,7 @@ extern "C" int blast_bsr_linear_scaled8(const blast_bsr_view* W, const blast_wei
   if (Y8) a.y8 = eight_of(Y8);
   if (Z8) a.k8[0] = eight_of(Z8);
   const bool exact = Y && !a.y_bf16;
-  if (W->b == 64) return exact ? launch_linear8<64, 128, false, true>(a, stream) : launch_linear8<64, 128, false, false>(a, stream);
-  return exact ? launch_linear8<128, 128, false, true>(a, stream) : launch_linear8<128, 128, false, false>(a, stream);
+  return W->b == 64 ? by_formats<64, false>(a, exact, stream) : by_formats<128, false>(a, exact, stream);
 }
 
 extern "C" int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_weight8_view* gate8, const blast_bsr_view* Wup,
@@ -126,5 +162,5 @@ extern "C" int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_
   if (H8) a.y8 = eight_of(H8);
   if (G8) a.k8[0] = eight_of(G8);
   if (U8) a.k8[1] = eight_of(U8);
-  return Wgate->b == 64 ? launch_linear8<64, 128, true, false>(a, stream) : launch_linear8<128, 128, true, false>(a, stream);
+  return Wgate->b == 64 ? by_formats<64, true>(a, false, stream) : by_formats<128, true>(a, false, stream);
 }

@@ -1,9 +1,12 @@
 // Products of scaled 8-bit operands (kern_scaled8.h) over the stored blocks of a block row: one matrix with bias, activation and
-// residual, or the gated pair; results in fp32, bf16 or scaled 8-bit form.
+// residual, or the gated pair; results in fp32, bf16 or scaled 8-bit form.  Features are the M dimension of the matrix instruction,
+// tokens the N dimension: a lane has one token and hands over its scale with the codes.
 //
-// A workgroup of four waves has a block row's B rows of TT tokens.  A step is 128 of the contraction: a stored block of 128 x 128
-// or two of 64 x 64, W and X tiles copied to LDS in rows of 128 bytes, the scales of the step's tokens beside them.  Features are the M
-// dimension of the matrix instruction, tokens the N dimension: a lane has one token and hands over its scale with the codes.
+// k_linear8: a workgroup of four waves has a block row's B rows of 128 tokens.  A step is 128 of the contraction: a stored block of
+// 128 x 128 or two of 64 x 64, W and X tiles copied to LDS in rows of 128 bytes, the scales of the step's tokens beside them; the next
+// step's copies are under way while one is multiplied.
+// k_linear8_split: eight waves have a block row's B rows of 32 tokens and deal the stored blocks among themselves, operands straight
+// into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
 #pragma once
 #include "kern_scaled8.h"
 #include "kern_stream.h"
@@ -26,6 +29,7 @@ struct Linear8Args {
   Eight x;
   int wfmt;
   int T, nbr, ntt;
+  int parts;             // XCDs that share a block row, each with its own token tiles: 1, 2, 4 or 8
   int act;
   const float* bias;     // single matrix: all of these
   const void* r;
@@ -94,94 +98,384 @@ __device__ __forceinline__ void linear8_finish(const Linear8Args& a, float (&z)[
   }
 }
 
-// One step of the contraction on 32 x 32 tiles: sixteen bytes twice of each operand's row are a lane's share of 64.
-template <int WF, int XF>
-__device__ __forceinline__ f32x16 mfma8(i32x8 w, i32x8 x, f32x16 c, int ws, int xs) {
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, WF, XF, 0, ws, 0, xs);
-}
 // The same codes widened to bf16, eight a 16-deep instruction.
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi, int fmt, float scale) {
   const u32x2v a = widen4((uint32_t)lo, fmt, scale), b = widen4((uint32_t)hi, fmt, scale);
   return __builtin_bit_cast(bf16x8, (u32x4{a[0], a[1], b[0], b[1]}));
 }
 
-template <int B, int TT, bool DUAL>
+// 64 of the contraction on 32 x 32 tiles: a lane has 32 bytes of a row of each operand, the same places on both.  EXACT: widened;
+// else in formats WF, XF.
+template <int RT, int NT, bool EXACT, int WF, int XF>
+__device__ __forceinline__ void multiply8(f32x16 (&d)[RT][NT], const i32x8 (&fw)[RT], const i32x8 (&fx)[NT], int ws, const int (&xs)[NT],
+                                          int wfmt, int xfmt) {
+  if constexpr (EXACT) {
+    const float wsf = scale_value(ws);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      bf16x8 bw[RT], bx[NT];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) bw[i] = widen8(fw[i][2 * p], fw[i][2 * p + 1], wfmt, wsf);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) bx[j] = widen8(fx[j][2 * p], fx[j][2 * p + 1], xfmt, scale_value(xs[j]));
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bw[i], bx[j], d[i][j], 0, 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        d[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[i], fx[j], d[i][j], WF, XF, 0, ws, 0, xs[j]);
+  }
+}
+
+// Workgroup ids go round the eight XCDs.  Each has every (8 / parts)th block row and one of `parts` runs of the token tiles, a row's tiles
+// one after the other.
+__device__ __forceinline__ bool place8(const Linear8Args& a, int& rank, int& tt) {
+  const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3, per = (a.ntt + a.parts - 1) / a.parts;
+  rank = k / per * (8 / a.parts) + xcd / a.parts;
+  tt = xcd % a.parts * per + k % per;
+  return rank < a.nbr && tt < a.ntt;
+}
+
+// Columns and scales of a block row's stored blocks, one a lane, 64 at a time.
+struct Blocks8 {
+  int col, scale;
+  __device__ __forceinline__ void load(const Mat8& m, int first, int n, int lane) {
+    col = scale = 0;
+    if (lane < n) {
+      col = m.col_idx[first + lane];
+      scale = m.scales[first + lane];
+    }
+  }
+};
+
+template <int B>
 struct L8Cfg {
   static_assert(B == 64 || B == 128, "");
+  static constexpr int NW = 4, NSTAGE = 2, TT = 32 * NW;  // tokens of a workgroup
   static constexpr int KB = 128 / B;            // stored blocks of a step
   static constexpr int WR = B / 64;             // waves along the rows, 64 each
-  static constexpr int WT = 4 / WR;             // waves along the tokens
+  static constexpr int WT = NW / WR;            // waves along the tokens
   static constexpr int TW = TT / WT;            // tokens of a wave
   static constexpr int NT = TW / 32;
   static constexpr int W_BYTES = B * 128, X_BYTES = TT * 128;
-  static constexpr int WI = W_BYTES / 4096, XI = X_BYTES / 4096;  // copy instructions of a wave, 1 KiB each
-  static constexpr int S_BYTES = 4 * 256;       // scales of the step's tokens: a wave copies those of one of its blocks
+  static constexpr int WI = W_BYTES / (1024 * NW), XI = X_BYTES / (1024 * NW);  // copy instructions of a wave, 1 KiB each
+  static constexpr int S_BYTES = KB * 256;
   static constexpr int STAGE = W_BYTES + X_BYTES + S_BYTES;
-  static constexpr int NSTAGE = 2;
-  static constexpr int EP_TOKENS = DUAL || TT * B * 4 > NSTAGE * STAGE ? TT / 2 : TT;  // tokens whose sums lie in LDS at once
-  static constexpr int EP_BYTES = EP_TOKENS * B * 4 * (DUAL ? 2 : 1);
-  static constexpr int LDS_BYTES = NSTAGE * STAGE > EP_BYTES ? NSTAGE * STAGE : EP_BYTES;
+  static constexpr int RING = NSTAGE * STAGE;
+  static constexpr int EX_BYTES = 3 * WR * TT * 4;  // largest magnitudes that the waves of a token's rows tell each other
+  static constexpr int LDS_BYTES = RING + EX_BYTES;
+  static constexpr int OUT_BYTES = 4096;            // a wave's part of a stage when results leave
+  static_assert(2 * B * TT + NW * OUT_BYTES <= RING && 3 * B * TT <= RING && LDS_BYTES <= 160 * 1024, "");
 };
 
-template <int B, int TT, bool DUAL, bool EXACT>
-__global__ __launch_bounds__(256) void k_linear8(const Linear8Args a) {
-  using C = L8Cfg<B, TT, DUAL>;
-  constexpr int NT = C::NT, KB = C::KB, NM = DUAL ? 2 : 1;
+// ---- results: a wave's 64 rows of 32 NT tokens, as the matrix instruction leaves them ----------------------------------------------
+//
+// Lane l has token l % 32 of a tile, register v row 8 (v / 4) + 4 (l / 32) + v % 4.  What leaves goes through a part of LDS that is the
+// wave's own, [token][row], so that neighbouring lanes store neighbouring bytes: 16-byte chunk c of a token lies at c ^ key(token).
+
+// f with the activation as a constant: decided once, not value by value.
+template <class F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == BLAST_ACT_SILU)
+    f(std::integral_constant<int, BLAST_ACT_SILU>{});
+  else if (act == BLAST_ACT_GELU)
+    f(std::integral_constant<int, BLAST_ACT_GELU>{});
+  else if (act == BLAST_ACT_RELU)
+    f(std::integral_constant<int, BLAST_ACT_RELU>{});
+  else
+    f(std::integral_constant<int, BLAST_ACT_NONE>{});
+}
+template <class A>
+__device__ __forceinline__ float act_of(A, float z) {
+  if constexpr (A::value == BLAST_ACT_NONE) return z;
+  return epilogue_act(A::value, z);
+}
+
+// Bits of the largest magnitude of a token's values, over the two lanes that share it.  As integers the positive values are in their
+// order and the negative ones, unsigned, above them in that of their magnitudes: two maxima and no sign taken off.  What is not finite
+// (beyond kMostBits) is left out when it turns out to be there.
+template <int NT>
+__device__ __forceinline__ void token_max(const f32x16 (&d)[2][NT], uint32_t (&m)[NT]) {
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    int p = 0;
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int w = __float_as_int(d[i][j][v]);
+        p = w > p ? w : p;
+        n = (uint32_t)w > n ? (uint32_t)w : n;
+      }
+    n &= 0x7FFFFFFFu;
+    uint32_t q = (uint32_t)p > n ? (uint32_t)p : n;
+    if (__any(q >= 0x7F800000u)) {
+      q = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const uint32_t u = magnitude(d[i][j][v]);
+          if (u < 0x7F800000u) q = u > q ? u : q;
+        }
+    }
+    const auto halves = __builtin_amdgcn_permlane32_swap(q, q, false, false);
+    m[j] = halves[0] > halves[1] ? halves[0] : halves[1];
+  }
+}
+
+// Codes of four values, a word.  CAP: finite magnitudes beyond kMostBits count as that.
+template <int FMT, bool CAP>
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float scale) {
+  if constexpr (CAP) {
+    auto cap = [](float x) {
+      const uint32_t u = magnitude(x);
+      return u > kMostBits && u < 0x7F800000u ? __builtin_copysignf(__uint_as_float(kMostBits), x) : x;
+    };
+    a = cap(a), b = cap(b), c = cap(c), d = cap(d);
+  }
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  s16x2 w = {0, 0};
+  if constexpr (FMT == BLAST_E4M3) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true);
+  } else {
+    w = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(w, a, b, scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(w, c, d, scale, true);
+  }
+  return __builtin_bit_cast(uint32_t, w);
+}
+
+// A workgroup's codes of one tensor meet in LDS, [token][row], so that a token's B bytes - a whole line of 128 - leave together and past
+// the L2s (bf16 results past the L2s too: 53248 x 16384 at 95 %, 2048 tokens 168 -> 146 us).
+template <int B>
+__device__ __forceinline__ uint32_t code_at(int tok, int chunk) {
+  return (uint32_t)(tok * B + ((chunk ^ (B == 128 ? tok & 7 : (tok >> 1) & 3)) << 4));
+}
+template <int B, int NT, int FMT>
+__device__ __forceinline__ void put_codes(const Eight& o, const f32x16 (&d)[2][NT], const uint32_t (&m)[NT], unsigned char* lds, int lane,
+                                          int tok0, int row, int64_t t0, int64_t T, int group) {
+  const int l32 = lane & 31, lh = lane >> 5;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int tok = tok0 + 32 * j + l32;
+    const int code = scale_code(m[j] > kMostBits ? kMostBits : m[j], FMT);
+    const float scale = scale_value(code);
+    if (row == 0 && lh == 0 && t0 + tok < T) o.scales[(int64_t)group * o.lds + t0 + tok] = (uint8_t)code;
+    auto tile = [&](auto cap) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<uint32_t*>(lds + code_at<B>(tok, (row >> 4) + 2 * i + (v >> 3)) + ((v & 4) ? 8 : 0) + 4 * lh) =
+              encode4<FMT, decltype(cap)::value>(d[i][j][v], d[i][j][v + 1], d[i][j][v + 2], d[i][j][v + 3], scale);
+    };
+    if (__any(m[j] > kMostBits))
+      tile(std::true_type{});
+    else
+      tile(std::false_type{});
+  }
+}
+// This wave's 64 rows (from `row` on) of tokens tok0 ... of the workgroup's tile, whose first is t0.
+template <int B, int NT>
+__device__ __forceinline__ void put_eight(const Eight& o, const f32x16 (&d)[2][NT], const uint32_t (&m)[NT], unsigned char* lds, int lane,
+                                          int tok0, int row, int64_t t0, int64_t T, int group) {
+  if (o.fmt == BLAST_E4M3)
+    put_codes<B, NT, BLAST_E4M3>(o, d, m, lds, lane, tok0, row, t0, T, group);
+  else
+    put_codes<B, NT, BLAST_E5M2>(o, d, m, lds, lane, tok0, row, t0, T, group);
+}
+// The tile's codes out of LDS, by all threads.
+template <int B, int TT>
+__device__ __forceinline__ void leave_eight(const Eight& o, const unsigned char* lds, int64_t t0, int64_t T, int64_t row0) {
+  constexpr int kLanes = B / 16, kTokens = 256 / kLanes;
+  const int c = threadIdx.x % kLanes;
+#pragma unroll
+  for (int k = 0; k < TT / kTokens; ++k) {
+    const int tok = k * kTokens + threadIdx.x / kLanes;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + code_at<B>(tok, c));
+    if (t0 + tok < T) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(o.codes + (t0 + tok) * o.ld + row0 + 16 * c));
+  }
+}
+
+template <int NT>
+__device__ __forceinline__ void put_bf16(uint16_t* y, int64_t ldy, bool vec, const f32x16 (&d)[2][NT], unsigned char* lds, int lane, int64_t t0,
+                                         int64_t T, int64_t row0) {
+  const int l32 = lane & 31, lh = lane >> 5, c = lane & 7;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4)
+        *reinterpret_cast<u32x2v*>(lds + l32 * 128 + (((4 * i + (v >> 2)) ^ (l32 & 7)) << 4) + 8 * lh) =
+            u32x2v{bf16_pair(d[i][j][v], d[i][j][v + 1]), bf16_pair(d[i][j][v + 2], d[i][j][v + 3])};
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int tok = 8 * k + (lane >> 3);
+      const int64_t t = t0 + 32 * j + tok;
+      const u32x4 w = *reinterpret_cast<const u32x4*>(lds + tok * 128 + ((c ^ (tok & 7)) << 4));
+      if (t < T) {
+        uint16_t* p = y + t * ldy + row0 + 8 * c;
+        if (vec) {
+          __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Four neighbouring rows of a token's residual.
+__device__ __forceinline__ void residual4(const Linear8Args& a, int64_t t, int64_t row, float (&r)[4]) {
+  if (a.r_bf16) {
+    const uint16_t* p = static_cast<const uint16_t*>(a.r) + t * a.ldr + row;
+    uint32_t w[2];
+    if (a.r_vec) {
+      const u32x2v q = *reinterpret_cast<const u32x2v*>(p);
+      w[0] = q[0], w[1] = q[1];
+    } else {
+      w[0] = p[0] | (uint32_t)p[1] << 16, w[1] = p[2] | (uint32_t)p[3] << 16;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = __uint_as_float(e % 2 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+  } else {
+    const float* p = static_cast<const float*>(a.r) + t * a.ldr + row;
+    if (a.r_vec) {
+      const float4 q = *reinterpret_cast<const float4*>(p);
+      r[0] = q.x, r[1] = q.y, r[2] = q.z, r[3] = q.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = p[e];
+    }
+  }
+}
+
+// Values of either type with their residual, 16 tokens at a time: a lane takes four neighbouring rows of a token, a token's 64 are
+// sixteen lanes'.
+template <int NT>
+__device__ __forceinline__ void put_sums(const Linear8Args& a, const f32x16 (&d)[2][NT], bool residual, unsigned char* lds, int lane,
+                                         int64_t t0, int64_t row0) {
+  const int l32 = lane & 31, lh = lane >> 5, c = lane & 15;
+#pragma unroll
+  for (int half = 0; half < 2 * NT; ++half) {
+    const int j = half >> 1;
+    const int64_t th = t0 + 16 * half;
+    float r[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[k][e] = 0.0f;
+      const int64_t t = th + 4 * k + (lane >> 4);
+      if (residual && t < a.T) residual4(a, t, row0 + 4 * c, r[k]);
+    }
+    if ((l32 >> 4) == (half & 1)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<float4*>(lds + (l32 & 15) * 256 + (((8 * i + (v >> 1) + lh) ^ (l32 & 7)) << 4)) =
+              float4{d[i][j][v], d[i][j][v + 1], d[i][j][v + 2], d[i][j][v + 3]};
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int tok = 4 * k + (lane >> 4);
+      const int64_t t = th + tok;
+      float4 w = *reinterpret_cast<const float4*>(lds + tok * 256 + ((c ^ (tok & 7)) << 4));
+      w.x += r[k][0], w.y += r[k][1], w.z += r[k][2], w.w += r[k][3];
+      if (t < a.T) {
+        if (a.y_bf16) {
+          uint16_t* p = static_cast<uint16_t*>(a.y) + t * a.ldy + row0 + 4 * c;
+          if (a.y_vec) {
+            *reinterpret_cast<u32x2v*>(p) = u32x2v{bf16_pair(w.x, w.y), bf16_pair(w.z, w.w)};
+          } else {
+            p[0] = f32_to_bf16_rne(w.x), p[1] = f32_to_bf16_rne(w.y), p[2] = f32_to_bf16_rne(w.z), p[3] = f32_to_bf16_rne(w.w);
+          }
+        } else {
+          float* p = static_cast<float*>(a.y) + t * a.ldy + row0 + 4 * c;
+          if (a.y_vec) {
+            *reinterpret_cast<float4*>(p) = w;
+          } else {
+            p[0] = w.x, p[1] = w.y, p[2] = w.z, p[3] = w.w;
+          }
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <int B, bool DUAL, bool EXACT, int WF, int XF>
+__global__ __launch_bounds__(256, B == 64 && !DUAL ? 3 : 2) void k_linear8(const Linear8Args a) {
+  using C = L8Cfg<B>;
+  constexpr int NW = C::NW, NT = C::NT, KB = C::KB, NM = DUAL ? 2 : 1, TT = C::TT;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l32 = lane & 31, lh = lane >> 5;
-  // ids go round the eight XCDs: the token tiles of a block row are eight apart, on one of them
-  const int id = blockIdx.x, span = 8 * a.ntt, rem = id % span;
-  const int rank = id / span * 8 + (rem & 7), tt = rem >> 3;
-  if (rank >= a.nbr) return;
-  const int r = a.row_order ? ld_idx(a.row_order, rank) : rank;
-  const int t0 = tt * TT;
   const int wr = wave / C::WT, wt = wave % C::WT;  // this wave's 64 rows and TW tokens
-
+  int rank, tt;
+  if (!place8(a, rank, tt)) return;
+  const int r = a.row_order ? ld_idx(a.row_order, rank) : rank, t0 = tt * TT;
   int kb[NM], nb[NM], steps[NM];
+  Blocks8 blocks[NM];
 #pragma unroll
   for (int m = 0; m < NM; ++m) {
     kb[m] = ld_idx(a.m[m].row_ptr, r);
     nb[m] = ld_idx(a.m[m].row_ptr, r + 1) - kb[m];
     steps[m] = (nb[m] + KB - 1) / KB;
   }
+#pragma unroll
+  for (int m = 0; m < NM; ++m) blocks[m].load(a.m[m], kb[m], nb[m], lane);
   const int total = steps[0] + (DUAL ? steps[NM - 1] : 0);
 
   // Copy side: position p (16 bytes) of a tile = row p / 8, slot p % 8; it holds chunk slot ^ row % 8 of that row's 128 bytes, which for
-  // two blocks are 64 of each.
+  // two blocks are 64 of each.  (row % 8 = lane / 8: a lane's chunk is the same in every instruction.)
+  const int chunk = (lane & 7) ^ ((lane >> 3) & 7);
+  const bool second = KB == 2 && chunk >= 4;  // it is of the second block
+  const uint32_t coff = KB == 2 ? (chunk & 3) * 16 : chunk * 16;
   uint32_t woff[C::WI];
+#pragma unroll
+  for (int i = 0; i < C::WI; ++i) woff[i] = (uint32_t)(((i * NW + wave) * 8 + (lane >> 3)) * B) + coff;
   const uint8_t* xrow[C::XI];
 #pragma unroll
-  for (int i = 0; i < C::WI; ++i) {
-    const int p = (i * 4 + wave) * 64 + lane, row = p >> 3, c = (p & 7) ^ (row & 7);
-    woff[i] = (uint32_t)(KB == 2 ? row * 64 + (c & 3) * 16 : row * 128 + c * 16);
-  }
-#pragma unroll
   for (int i = 0; i < C::XI; ++i) {
-    const int p = (i * 4 + wave) * 64 + lane, row = p >> 3, c = (p & 7) ^ (row & 7);
-    int t = t0 + row;
+    int t = t0 + (i * NW + wave) * 8 + (lane >> 3);
     t = t < a.T ? t : a.T - 1;  // rows beyond the last token read it again; nothing of them is stored
-    xrow[i] = a.x.codes + t * a.x.ld + (KB == 2 ? (c & 3) * 16 : c * 16);
+    xrow[i] = a.x.codes + t * a.x.ld + coff;
   }
   int64_t soff = t0 + 4 * (lane < TT / 4 ? lane : TT / 4 - 1);
   soff = soff < a.x.lds - 4 ? soff : a.x.lds - 4;
-  const bool second = KB == 2 && (((lane & 7) ^ ((lane >> 3) & 7)) >= 4);  // (row % 8 = lane / 8: this lane's chunk is of the second block)
 
   auto issue = [&](int m, int s, int slot) {
     unsigned char* st = smem + slot * C::STAGE;
-    const int q0 = kb[m] + s * KB;
-    const int q1 = KB == 2 && s * KB + 1 < nb[m] ? q0 + 1 : q0;
-    const int c0 = ld_idx(a.m[m].col_idx, q0), c1 = KB == 2 ? ld_idx(a.m[m].col_idx, q1) : c0;
+    const int b0 = s * KB;
+    if (b0 > 0 && (b0 & 63) == 0) blocks[m].load(a.m[m], kb[m] + b0, nb[m] - b0, lane);
+    const bool two = KB == 2 && b0 + 1 < nb[m];
+    const int c0 = __builtin_amdgcn_readlane(blocks[m].col, b0 & 63);
+    const int c1 = two ? __builtin_amdgcn_readlane(blocks[m].col, (b0 + 1) & 63) : c0;
+    const int q0 = kb[m] + b0, q1 = two ? q0 + 1 : q0;
     const uint8_t* wsrc = a.m[m].vals + (int64_t)(second ? q1 : q0) * (B * B);
     const int64_t xcol = (int64_t)(second ? c1 : c0) * B;
 #pragma unroll
-    for (int i = 0; i < C::WI; ++i) BLAST_GLDS16(wsrc + woff[i], st + (i * 4 + wave) * 1024);
+    for (int i = 0; i < C::WI; ++i) BLAST_GLDS16(wsrc + woff[i], st + (i * NW + wave) * 1024);
 #pragma unroll
-    for (int i = 0; i < C::XI; ++i) BLAST_GLDS16(xrow[i] + xcol, st + C::W_BYTES + (i * 4 + wave) * 1024);
-    const int cs = KB == 2 && (wave & 1) ? c1 : c0;
+    for (int i = 0; i < C::XI; ++i) BLAST_GLDS16(xrow[i] + xcol, st + C::W_BYTES + (i * NW + wave) * 1024);
+    // (every wave copies the scales of one of the step's blocks: those that copy the same write the same)
+    const int which = wave % KB, cs = which ? c1 : c0;
     __builtin_amdgcn_global_load_lds(
         (const __attribute__((address_space(1))) void*)(a.x.scales + (((int64_t)cs * B) >> a.x.shift) * a.x.lds + soff),
-        (__attribute__((address_space(3))) void*)(st + C::W_BYTES + C::X_BYTES + wave * 256), 4, 0, 0);
+        (__attribute__((address_space(3))) void*)(st + C::W_BYTES + C::X_BYTES + which * 256), 4, 0, 0);
   };
 
   f32x16 acc[NM][2][NT];
@@ -196,15 +490,12 @@ __global__ __launch_bounds__(256) void k_linear8(const Linear8Args a) {
 
   // Fragment side: of each 64 of a row lane half h takes chunks h and h + 2, the same on both operands.
   auto chunk_at = [&](int row, int c) { return (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4)); };
-  auto multiply = [&](f32x16 (&d)[2][NT], int m, int s, int slot) {
+  auto multiply = [&](f32x16 (&d)[2][NT], int w0, int w1, bool two, int slot) {
     const unsigned char* st = smem + slot * C::STAGE;
     const unsigned char* sc = st + C::W_BYTES + C::X_BYTES;
-    const int q0 = kb[m] + s * KB;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      if (KB == 2 && kk == 1 && s * KB + 1 >= nb[m]) break;  // (an odd number of blocks)
-      const int q = q0 + (KB == 2 ? kk : 0);
-      const int ws = (ld_idx(reinterpret_cast<const int*>(a.m[m].scales), q >> 2) >> (8 * (q & 3))) & 255;  // (through the scalar unit)
+      if (KB == 2 && kk == 1 && !two) break;  // (an odd number of blocks)
       i32x8 fw[2], fx[NT];
       int xs[NT];
 #pragma unroll
@@ -222,104 +513,261 @@ __global__ __launch_bounds__(256) void k_linear8(const Linear8Args a) {
         fx[j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         xs[j] = sc[(KB == 2 ? kk : 0) * 256 + row];
       }
-      if constexpr (EXACT) {
-        const float wsf = scale_value(ws);
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          bf16x8 bw[2], bx[NT];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) bw[i] = widen8(fw[i][2 * p], fw[i][2 * p + 1], a.wfmt, wsf);
-#pragma unroll
-          for (int j = 0; j < NT; ++j) bx[j] = widen8(fx[j][2 * p], fx[j][2 * p + 1], a.x.fmt, scale_value(xs[j]));
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bw[i], bx[j], d[i][j], 0, 0, 0);
-        }
-      } else {
-        auto all = [&](auto wf, auto xf) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) d[i][j] = mfma8<wf.value, xf.value>(fw[i], fx[j], d[i][j], ws, xs[j]);
-        };
-        using F0 = std::integral_constant<int, 0>;
-        using F1 = std::integral_constant<int, 1>;
-        if (a.wfmt == BLAST_E4M3) {
-          if (a.x.fmt == BLAST_E4M3)
-            all(F0{}, F0{});
-          else
-            all(F0{}, F1{});
-        } else {
-          if (a.x.fmt == BLAST_E4M3)
-            all(F1{}, F0{});
-          else
-            all(F1{}, F1{});
-        }
-      }
+      multiply8<2, NT, EXACT, WF, XF>(d, fw, fx, kk && KB == 2 ? w1 : w0, xs, a.wfmt, a.x.fmt);
     }
   };
 
-  auto issue_step = [&](int g, int slot) {
+  // The two matrices' steps are one sequence; what a step multiplies by is read from its blocks' lanes before the next one is issued.
+  auto issue_step = [&](int g) {
     if (!DUAL || g < steps[0])
-      issue(0, g, slot);
+      issue(0, g, g & 1);
     else
-      issue(NM - 1, g - steps[0], slot);
+      issue(NM - 1, g - steps[0], g & 1);
   };
-  if (total > 0) issue_step(0, 0);
+  auto run = [&](int m, f32x16 (&d)[2][NT], int base) {
 #pragma unroll 1
-  for (int g = 0; g < total; ++g) {
-    __syncthreads();  // (waits for this wave's copies: step g's have landed, everybody has read step g - 1)
-    if (g + 1 < total) issue_step(g + 1, (g + 1) & 1);
-    if (!DUAL || g < steps[0])
-      multiply(acc[0], 0, g, g & 1);
-    else
-      multiply(acc[NM - 1], NM - 1, g - steps[0], g & 1);
+    for (int s = 0; s < steps[m]; ++s) {
+      const int g = base + s, b0 = s * KB;
+      const bool two = KB == 2 && b0 + 1 < nb[m];
+      const int w0 = __builtin_amdgcn_readlane(blocks[m].scale, b0 & 63), w1 = __builtin_amdgcn_readlane(blocks[m].scale, (b0 + 1) & 63);
+      __builtin_amdgcn_s_waitcnt(BLAST_VMCNT(0));  // this wave's copies of the step have landed (a barrier need not wait for a copy)
+      __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): what was read of the step before is here
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();  // so have everybody's, and the stage of the step before is free
+      asm volatile("" ::: "memory");
+      if (g + 1 < total) issue_step(g + 1);
+      multiply(d, w0, w1, two, g & 1);
+    }
+  };
+  if (total > 0) issue_step(0);
+  run(0, acc[0], 0);
+  if constexpr (DUAL) run(1, acc[NM - 1], steps[0]);
+
+  // Results, by way of the ring, whose last step a barrier below has seen read.  `ex`: largest magnitudes over a wave's rows of each
+  // token, of up to three tensors; a group of 128 rows is two waves'.
+  unsigned char* lds = smem + 2 * B * TT + wave * C::OUT_BYTES;  // (behind the codes of two tensors)
+  uint32_t* ex = reinterpret_cast<uint32_t*>(smem + C::RING);
+  const int64_t tw = t0 + wt * C::TW, row0 = (int64_t)r * B + wr * 64;
+  auto tell = [&](int k, const uint32_t (&m)[NT]) {
+    if (lh == 0) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) ex[(k * C::WR + wr) * TT + wt * C::TW + 32 * j + l32] = m[j];
+    }
+  };
+  auto told = [&](int k, uint32_t (&m)[NT]) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      m[j] = 0;
+#pragma unroll
+      for (int w = 0; w < C::WR; ++w) {
+        const uint32_t o = ex[(k * C::WR + w) * TT + wt * C::TW + 32 * j + l32];
+        m[j] = o > m[j] ? o : m[j];
+      }
+    }
+  };
+  constexpr int kCodes = B * TT;  // bytes of the tile's codes
+  const int tok0 = wt * C::TW;
+  const int64_t rows0 = (int64_t)r * B;
+  if constexpr (DUAL) {
+    const bool keep_g = a.k8[0].codes, keep_u = a.k8[1].codes, to8 = a.y8.codes;
+    uint32_t m[NT];
+    if (keep_g) token_max<NT>(acc[0], m), tell(0, m);
+    if (keep_u) token_max<NT>(acc[1], m), tell(1, m);
+    __syncthreads();  // (everybody has read the last step; what was told can be heard)
+    if (keep_g) told(0, m), put_eight<B, NT>(a.k8[0], acc[0], m, smem, lane, tok0, wr * 64, t0, a.T, r);
+    if (keep_u) told(1, m), put_eight<B, NT>(a.k8[1], acc[1], m, smem + kCodes, lane, tok0, wr * 64, t0, a.T, r);
+    f32x16 (&h)[2][NT] = acc[0];
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) h[i][j][v] = act_of(act, h[i][j][v]) * acc[1][i][j][v];
+    });
+    if (to8) token_max<NT>(h, m), tell(2, m);
+    __syncthreads();  // (G's and U's codes are in LDS)
+    if (keep_g) leave_eight<B, TT>(a.k8[0], smem, t0, a.T, rows0);
+    if (keep_u) leave_eight<B, TT>(a.k8[1], smem + kCodes, t0, a.T, rows0);
+    if (to8) {
+      told(2, m), put_eight<B, NT>(a.y8, h, m, smem + 2 * kCodes, lane, tok0, wr * 64, t0, a.T, r);
+      __syncthreads();
+      leave_eight<B, TT>(a.y8, smem + 2 * kCodes, t0, a.T, rows0);
+    } else {
+      put_bf16<NT>(static_cast<uint16_t*>(a.y), a.ldy, a.y_vec, h, lds, lane, tw, a.T, row0);
+    }
+  } else {
+    f32x16 (&d)[2][NT] = acc[0];
+    if (a.bias) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const float b = a.bias[row0 + 32 * i + 8 * (v >> 2) + 4 * lh + (v & 3)];
+#pragma unroll
+          for (int j = 0; j < NT; ++j) d[i][j][v] += b;
+        }
+    }
+    const bool keep = a.k8[0].codes, to8 = a.y8.codes;
+    uint32_t m[NT];
+    if (keep) token_max<NT>(d, m), tell(0, m);
+    __syncthreads();  // (everybody has read the last step; what was told can be heard)
+    if (keep) {
+      told(0, m), put_eight<B, NT>(a.k8[0], d, m, smem, lane, tok0, wr * 64, t0, a.T, r);
+      __syncthreads();
+      leave_eight<B, TT>(a.k8[0], smem, t0, a.T, rows0);
+    }
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) d[i][j][v] = act_of(act, d[i][j][v]);
+    });
+    const bool added = to8 && a.r;  // (before the result is written: it may be where the residual is)
+    if (added) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int64_t t = tw + 32 * j + l32;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int v = 0; v < 16; v += 4) {
+            float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (t < a.T) residual4(a, t, row0 + 32 * i + 2 * v + 4 * lh, q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[i][j][v + e] += q[e];
+          }
+      }
+    }
+    if (a.y) {
+      if (!a.y_bf16 || (a.r && !added))
+        put_sums<NT>(a, d, a.r && !added, lds, lane, tw, row0);
+      else
+        put_bf16<NT>(static_cast<uint16_t*>(a.y), a.ldy, a.y_vec, d, lds, lane, tw, a.T, row0);
+    }
+    if (to8) {
+      token_max<NT>(d, m), tell(1, m);
+      __syncthreads();
+      told(1, m), put_eight<B, NT>(a.y8, d, m, smem + kCodes, lane, tok0, wr * 64, t0, a.T, r);
+      __syncthreads();
+      leave_eight<B, TT>(a.y8, smem + kCodes, t0, a.T, rows0);
+    }
+  }
+}
+
+// ---- few tiles: waves share the stored blocks of a block row ------------------------------------------------------------------
+
+template <int B, bool DUAL>
+struct S8Cfg {
+  static constexpr int NW = 8, TT = 32, RT = B / 32;
+  static constexpr int EP_TOKENS = DUAL && B == 128 ? 16 : 32;  // tokens whose sums lie in LDS at once, of every wave and matrix
+  static constexpr int LDS_BYTES = NW * EP_TOKENS * B * 4 * (DUAL ? 2 : 1);
+};
+
+template <int B, bool DUAL, bool EXACT, int WF, int XF>
+__global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
+  using C = S8Cfg<B, DUAL>;
+  constexpr int NM = DUAL ? 2 : 1, RT = C::RT, NW = C::NW, KS = B / 64;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int l32 = lane & 31, lh = lane >> 5;
+  int rank, tt;
+  if (!place8(a, rank, tt)) return;
+  const int r = a.row_order ? ld_idx(a.row_order, rank) : rank;
+  const int t0 = tt * C::TT;
+  int kb[NM], nb[NM];
+#pragma unroll
+  for (int m = 0; m < NM; ++m) {
+    kb[m] = ld_idx(a.m[m].row_ptr, r);
+    nb[m] = ld_idx(a.m[m].row_ptr, r + 1) - kb[m];
+  }
+  const int64_t t = t0 + l32 < a.T ? t0 + l32 : a.T - 1;  // (lanes beyond the last token repeat it; nothing of them is stored)
+  const uint8_t* xrow = a.x.codes + t * a.x.ld + lh * 32;
+
+  f32x16 acc[NM][RT][1];
+#pragma unroll
+  for (int m = 0; m < NM; ++m)
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[m][i][0][v] = 0.0f;
+
+  auto block = [&](f32x16 (&d)[RT][1], const Mat8& m, int q) {
+    const int c = ld_idx(m.col_idx, q);
+    const int ws = (ld_idx(reinterpret_cast<const int*>(m.scales), q >> 2) >> (8 * (q & 3))) & 255;
+    const uint8_t* w = m.vals + (int64_t)q * (B * B) + l32 * B + lh * 32;
+    const uint8_t* x = xrow + (int64_t)c * B;
+    const int xs[1] = {a.x.scales[(((int64_t)c * B) >> a.x.shift) * a.x.lds + t]};
+    i32x8 fw[KS][RT], fx[KS][1];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const i32x4* p = reinterpret_cast<const i32x4*>(w + i * 32 * B + k * 64);
+        fw[k][i] = __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+      const i32x4* p = reinterpret_cast<const i32x4*>(x + k * 64);
+      fx[k][0] = __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+#pragma unroll
+    for (int k = 0; k < KS; ++k) multiply8<RT, 1, EXACT, WF, XF>(d, fw[k], fx[k], ws, xs, a.wfmt, a.x.fmt);
+  };
+  // the blocks of both matrices are dealt as one sequence
+#pragma unroll 1
+  for (int e = wave; e < nb[0]; e += NW) block(acc[0], a.m[0], kb[0] + e);
+  if constexpr (DUAL) {
+#pragma unroll 1
+    for (int e = (wave + NW - nb[0] % NW) % NW; e < nb[1]; e += NW) block(acc[1], a.m[1], kb[1] + e);
   }
 
-  // The sums through LDS, [token][row] in fp32, so that a lane ends with eight neighbouring rows of a token: 16-byte chunk c of a token
-  // lies at c ^ token % 8.
-  constexpr int kPieces = B / 8, kRows = 256 / kPieces, PITCH = B * 4;
+  const int all = nb[0] + (DUAL ? nb[NM - 1] : 0), waves = all < NW ? (all < 1 ? 1 : all) : NW;  // those that have sums
+  constexpr int kPieces = B / 8, kRows = 64 * NW / kPieces, PITCH = B * 4, SET = C::EP_TOKENS * PITCH;
   const int piece = threadIdx.x % kPieces;
   const int64_t row = (int64_t)r * B + piece * 8;
   float bias[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) bias[j] = !DUAL && a.bias ? a.bias[row + j] : 0.0f;
 #pragma unroll
-  for (int pass = 0; pass < TT / C::EP_TOKENS; ++pass) {
-    __syncthreads();
+  for (int pass = 0; pass < C::TT / C::EP_TOKENS; ++pass) {
+    if (t0 + pass * C::EP_TOKENS >= a.T) break;
+    if (pass > 0) __syncthreads();
+    const int tok = l32 - pass * C::EP_TOKENS;
+    if (wave < waves && tok >= 0 && tok < C::EP_TOKENS) {
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+      for (int m = 0; m < NM; ++m) {
+        unsigned char* base = smem + (wave * NM + m) * SET + tok * PITCH;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int tok = wt * C::TW + 32 * j + l32 - pass * C::EP_TOKENS;
-        if (tok >= 0 && tok < C::EP_TOKENS) {
-          unsigned char* base = smem + m * (C::EP_TOKENS * PITCH) + tok * PITCH;
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int v = 0; v < 16; v += 4) {
-              const int c = (wr * 64 + 32 * i + 2 * v + 4 * lh) / 4;
-              *reinterpret_cast<float4*>(base + ((c ^ (tok & 7)) << 4)) =
-                  float4{acc[m][i][j][v], acc[m][i][j][v + 1], acc[m][i][j][v + 2], acc[m][i][j][v + 3]};
-            }
-        }
+          for (int v = 0; v < 16; v += 4) {
+            const int c = (32 * i + 2 * v + 4 * lh) / 4;
+            *reinterpret_cast<float4*>(base + ((c ^ (tok & 7)) << 4)) =
+                float4{acc[m][i][0][v], acc[m][i][0][v + 1], acc[m][i][0][v + 2], acc[m][i][0][v + 3]};
+          }
       }
+    }
     __syncthreads();
 #pragma unroll 1
-    for (int tok = threadIdx.x / kPieces; tok < C::EP_TOKENS; tok += kRows) {
-      const int64_t t = t0 + pass * C::EP_TOKENS + tok;
-      if (t0 + pass * C::EP_TOKENS + (tok & ~(kRows - 1)) >= a.T) break;  // (the same for the workgroup)
+    for (int k = threadIdx.x / kPieces; k < C::EP_TOKENS; k += kRows) {
+      const int64_t tk = t0 + pass * C::EP_TOKENS + k;
+      if (t0 + pass * C::EP_TOKENS + (k & ~(kRows - 1)) >= a.T) break;
       float z[8], u[8];
-      auto take = [&](int m, float (&v)[8]) {
-        const unsigned char* base = smem + m * (C::EP_TOKENS * PITCH) + tok * PITCH;
-        const float4 lo = *reinterpret_cast<const float4*>(base + (((2 * piece) ^ (tok & 7)) << 4));
-        const float4 hi = *reinterpret_cast<const float4*>(base + (((2 * piece + 1) ^ (tok & 7)) << 4));
-        v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+      auto take = [&](int m, float (&v)[8]) {  // the waves' sums in their order
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+#pragma unroll 1
+        for (int w = 0; w < waves; ++w) {
+          const unsigned char* base = smem + (w * NM + m) * SET + k * PITCH;
+          const float4 lo = *reinterpret_cast<const float4*>(base + (((2 * piece) ^ (k & 7)) << 4));
+          const float4 hi = *reinterpret_cast<const float4*>(base + (((2 * piece + 1) ^ (k & 7)) << 4));
+          v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w, v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
+        }
       };
       take(0, z);
       if constexpr (DUAL) take(1, u);
-      linear8_finish<B, DUAL>(a, z, u, bias, t, row, t < a.T);
+      linear8_finish<B, DUAL>(a, z, u, bias, tk, row, tk < a.T);
     }
   }
 }

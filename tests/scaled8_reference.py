@@ -69,15 +69,24 @@ def quantised(x, group, fmt):
     T, K = x.shape
     x = np.where(np.isfinite(x), np.clip(x, -MOST, MOST), x)
     n = -(-K // group)
-    codes, scales = np.zeros((T, K), np.uint8), np.zeros((n, T), np.uint8)
-    for g in range(n):
-        part = x[:, g * group:(g + 1) * group]
-        for t in range(T):
-            fine = np.abs(part[t][np.isfinite(part[t])])
-            e = exponent(fine.max() if fine.size else 0.0, fmt)
-            scales[g, t] = e + 127
-            codes[t, g * group:(g + 1) * group] = encode(part[t] / 2.0 ** e, fmt)
-    return codes, scales
+    w = np.zeros((T, n * group))
+    w[:, :K] = x
+    w = w.reshape(T, n, group)
+    most = np.abs(np.where(np.isfinite(w), w, 0.0)).max(2)
+    e = exponents(most, fmt)
+    codes = encode(np.ldexp(w, -e[:, :, None]), fmt).reshape(T, n * group)[:, :K]
+    return codes, (e + 127).astype(np.uint8).T
+
+
+def exponents(most, fmt):
+    """exponent() of every value of an array: a candidate from the logarithm, put right by the definition's own comparison."""
+    largest = FORMATS[fmt][2]
+    e = np.full(most.shape, -100, dtype=np.int64)
+    some = most > 0
+    e[some] = np.maximum(np.floor(np.log2(most[some] / largest)).astype(np.int64) - 1, -100)
+    for _ in range(4):
+        e += most > np.ldexp(largest, e)
+    return e
 
 
 def same_codes(got, want, fmt):

@@ -59,13 +59,17 @@ class Matrix:
             self.dense[r * b:(r + 1) * b, c * b:(c + 1) * b] = torch.from_numpy(ref.table(fmt)[want] * 2.0 ** e)
 
     def product(self, x):
-        """W x^T as [T, rows], and how far the widened and the 8-bit instruction's sums may be off."""
-        z = x @ self.dense.t()
-        n = int((self.dense != 0).sum(1).max()) if self.where else 0
-        wide = n * 2.0 ** -24 * (x.abs() @ self.dense.abs().t())
-        wm = self.dense.abs().view(self.rows, -1, 64).amax(2)
+        """W x^T as [T, rows], and how far the widened and the 8-bit instruction's sums may be off (products of 64-bit matrices, made on
+        the GPU: nothing of the library)."""
+        x, w = x.cuda(), self.dense.cuda()
+        wt = w.t().contiguous()
+        z = torch.matmul(x, wt)
+        n = int((w != 0).sum(1).max()) if self.where else 0
+        wide = n * 2.0 ** -24 * torch.matmul(x.abs(), wt.abs())
+        wm = w.abs().view(self.rows, -1, 64).amax(2)
         xm = x.abs().view(x.shape[0], -1, 64).amax(2)
-        return z, wide, wide + 64 * 2.0 ** -15 * (xm @ wm.t())
+        low = wide + 64 * 2.0 ** -15 * torch.matmul(xm, wm.t().contiguous())
+        return z.cpu(), wide.cpu(), low.cpu()
 
 
 def masks(nr, nc, seed, keep=0.4):
@@ -267,6 +271,118 @@ def test_gated(b, T, act, out, keep):
         close(r.H, h, off + 2.0 ** -8 * (h.abs() + off))
     else:
         close8(r.H, h, off, "H")
+
+
+# 25 block rows of 17 tiles of 128 tokens, the last of 52: calls with work for every CU
+MANY = (25, 3, 2100)
+
+
+@pytest.mark.parametrize("b,fmts", [(64, ("e4m3", "e4m3")), (128, ("e4m3", "e4m3")), (64, ("e5m2", "e4m3")), (128, ("e4m3", "e5m2")), (64, ("e5m2", "e5m2"))])
+@pytest.mark.parametrize("act,residual,out,pre", [(None, None, "f32", False), (None, None, "bf16", False), ("gelu", "f32", "f32", True),
+                                                  ("silu", "bf16", "bf16", False), ("relu", None, "e4m3", True), (None, "bf16", "e4m3", False)])
+def test_product_of_many_tiles(b, fmts, act, residual, out, pre):
+    nr, nc, T = MANY
+    g = gen(b + len(out))
+    m = Matrix(g, masks(nr, nc, 5, 0.6), b, fmts[0])
+    q, x = eight(activation(g, T, m.cols, 0.3), b, fmts[1])
+    z, wide, low = m.product(x)
+    r = None if residual is None else torch.randn((T, m.rows), generator=g).to(F32 if residual == "f32" else BF16)
+    bias = torch.randn((m.rows,), generator=g) * 0.3
+    kept = api.empty_scaled8(T, m.rows, group=b) if pre else None
+    how = {"out_fmt": out} if out == "e4m3" else {"out_dtype": F32 if out == "f32" else BF16}
+    y = api.bsr_linear_scaled8(m.w8, q, bias=bias.cuda(), act=act, residual=None if r is None else r.cuda(), pre=kept, **how)
+    off = (wide if out == "f32" else low) + 2.0 ** -22 * (z.abs() + bias.abs())
+    z = z + bias.double()
+    if pre:
+        close8(kept, z, off, "kept")
+    v, off = ref.act(act, z), 1.13 * off + 2.0 ** -20 * z.abs()
+    if r is not None:
+        v, off = v + r.double(), off + 2.0 ** -23 * (v.abs() + r.abs())
+    if out == "e4m3":
+        close8(y, v, off)
+    else:
+        close(y, v, off + (2.0 ** -24 if out == "f32" else 2.0 ** -8) * (v.abs() + off))
+
+
+@pytest.mark.parametrize("b", [64, 128])
+@pytest.mark.parametrize("act,out,keep", [("silu", "e4m3", True), ("gelu", "bf16", True), (None, "e5m2", False)])
+def test_gated_of_many_tiles(b, act, out, keep):
+    nr, nc, T = MANY
+    g = gen(b)
+    mg, mu = (Matrix(g, masks(nr, nc, s, 0.6), b, "e4m3") for s in (1, 2))
+    q, x = eight(activation(g, T, mg.cols, 0.3), 128, "e4m3")
+    r = api.bsr_gated_scaled8(mg.w8, mu.w8, q, act=act, keep=keep, out_fmt=None if out == "bf16" else out)
+    (zg, _, og), (zu, _, ou) = mg.product(x), mu.product(x)
+    if keep:
+        close8(r.G, zg, og, "G")
+        close8(r.U, zu, ou, "U")
+    a = ref.act(act, zg)
+    h = a * zu
+    off = (1.13 * og + 2.0 ** -20 * zg.abs()) * (zu.abs() + ou) + a.abs() * ou + 2.0 ** -23 * h.abs()
+    if out == "bf16":
+        close(r.H, h, off + 2.0 ** -8 * (h.abs() + off))
+    elif out == "e4m3":
+        close8(r.H, h, off, "H")
+    else:
+        _, s = ref.quantised(h.numpy(), b, out)
+        scale = torch.from_numpy(np.ldexp(1.0, s.astype(np.int64) - 127).T).repeat_interleave(b, 1)
+        close(torch.from_numpy(ref.values(r.H.codes, r.H.scales, b, out)), h, off + 2.0 ** -3 * (h.abs() + off) + 2.0 ** -16 * scale)
+
+
+@pytest.mark.parametrize("b", [64, 128])
+@pytest.mark.parametrize("tiles", [1, 17])
+def test_results_are_rounded_like_the_quantiser(b, tiles):
+    """Integers: sums are exact whatever the instruction, and so the codes and scales of what a product writes are those of its fp32
+    result through the quantiser - zeros, negative zeros, and with infinities and NaN in some tokens too."""
+    T = 128 * tiles - 5
+    g = gen(b)
+    nr = 25 if tiles > 1 else 3
+    w = torch.randint(-3, 4, (nr * b, 3 * b), generator=g).to(BF16)
+    p = api.bsr_pack(w.cuda(), b, mask=masks(nr, 3, 8, 0.6).cuda())
+    w8 = api.bsr_quantize_scaled8(p)
+    xf = torch.randint(-4, 5, (T, 3 * b), generator=g).float()
+    xf[:, :b] *= (torch.rand((T, 1), generator=g) < 0.5)
+    for special in (False, True):
+        if special:
+            xf[1, 3], xf[2, b + 1], xf[5, 2 * b] = float("inf"), float("nan"), float("-inf")
+        x = api.quantize_scaled8(xf.cuda(), group=b, fmt="e5m2")
+        y = api.bsr_linear_scaled8(w8, x)
+        if not special:
+            assert torch.equal(y.cpu().double(), xf.double() @ api.bsr_unpack(p).cpu().double().t())
+        for fmt in ("e4m3", "e5m2"):
+            want = api.quantize_scaled8(y, group=b, fmt=fmt)
+            pre = api.empty_scaled8(T, nr * b, group=b, fmt=fmt)
+            got = api.bsr_linear_scaled8(w8, x, out_fmt=fmt, pre=pre)
+            for q in (got, pre):
+                assert torch.equal(q.scales[:, :T], want.scales[:, :T])
+                assert ref.same_codes(q.codes.cpu().numpy(), want.codes.cpu().numpy(), fmt)
+            h = api.empty_scaled8(T, nr * b, group=b, fmt=fmt)
+            api.bsr_gated_scaled8(w8, w8, x, act=None, out=h)
+            square = api.quantize_scaled8(y * y, group=b, fmt=fmt)
+            assert torch.equal(h.scales[:, :T], square.scales[:, :T])
+            assert ref.same_codes(h.codes.cpu().numpy(), square.codes.cpu().numpy(), fmt)
+
+
+def test_residual_under_the_result_and_codes_beside_it():
+    """Y on its residual's place and the same values in 8 bits, by the C call."""
+    import ctypes as C
+
+    for b, T in ((64, 37), (128, 2100)):
+        g = gen(b)
+        nr = 4 if T < 100 else 25
+        m = Matrix(g, masks(nr, 3, 3), b, "e4m3")
+        q, _ = eight(activation(g, T, m.cols, 0.3), b, "e4m3")
+        h = torch.randn((T, m.rows), generator=g).cuda()
+        want = api.bsr_linear_scaled8(m.w8, q, residual=h)
+        y8 = api.empty_scaled8(T, m.rows, group=b)
+        v, w, x, o = m.packed.view(), m.w8.view(), q.view(), y8.view()
+        rc = api.lib().blast_bsr_linear_scaled8(C.byref(v), C.byref(w), C.byref(x), T, None, -1, h.data_ptr(), m.rows, api.F32, h.data_ptr(),
+                                                m.rows, api.F32, C.byref(o), None, torch.cuda.current_stream().cuda_stream)
+        assert rc == 0
+        torch.cuda.synchronize()
+        assert torch.equal(h, want)
+        again = api.quantize_scaled8(want, group=b)
+        assert torch.equal(y8.codes, again.codes) and torch.equal(y8.scales[:, :T], again.scales[:, :T])
 
 
 def test_empty_matrix_no_tokens_and_one_block():

@@ -183,4 +183,5 @@ def test_reference_exponent_by_brute_force():
     for fmt in ref.FORMATS:
         for m in [448.0, 448.0000001, 57344.0, 57345.0, 1.0, 1.75, 1.7500001, 0.875, 2.0 ** -126, 3e38, 2.0 ** -100]:
             want = next(e for e in range(-100, 130) if m <= ref.FORMATS[fmt][2] * 2.0 ** e)
-            assert ref.exponent(m, fmt) == want
+            assert ref.exponent(m, fmt) == want and ref.exponents(np.array([m]), fmt)[0] == want
+        assert ref.exponents(np.array([0.0]), fmt)[0] == -100
