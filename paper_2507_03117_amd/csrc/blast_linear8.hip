@@ -8,8 +8,11 @@ using namespace blast_dev;
 
 namespace {
 
-// Fewer 128-token tiles than this are cut into tiles of 32 whose blocks eight waves share.
-constexpr int64_t kFewTiles = 384;
+// Fewer 128-token tiles than this are cut into tiles of 32 whose blocks eight waves share, and up to 32 tokens any number.  Microseconds
+// of 128-token tiles / of 32, with the number of the former: 2048 x 8192 at 90 %, 64-wide, fp32, 16 tiles 12.2 / 6.6, 64: 14.5 / 9.3, 128:
+// 15.0 / 11.5, 256: 16.6 / 20.2; 1600 x 6400 at 80 %, 75: 17.7 / 11.0, 200: 18.5 / 20.0; 4096 x 14336 at 95 %, 128-wide, bf16, 64: 11.0 /
+// 10.2, 256: 12.3 / 27.5; gated, 8192 x 2048 at 90 %, 128: 9.4 / 6.8, 256: 10.9 / 21.5; 14336 x 4096 at 95 %, 112: 13.6 / 14.7.
+constexpr int64_t kFewTiles = 144;
 
 int check_weight(const blast_bsr_view* W, const blast_weight8_view* W8) {
   if (!W || !W->row_ptr || !W8 || !format8_ok(W8->format)) return BLAST_ERR_INVALID_ARG;
@@ -74,13 +77,11 @@ int launch_linear8(Linear8Args a, hipStream_t stream) {
   return BLAST_OK;
 }
 
-template <int B, bool DUAL>
-int by_formats(const Linear8Args& a, bool exact, hipStream_t stream) {
-  if constexpr (!DUAL)
-    if (exact) return launch_linear8<B, DUAL, true, 0, 0>(a, stream);
+template <int B, bool DUAL, bool EXACT>
+int by_formats(const Linear8Args& a, hipStream_t stream) {
   if (a.wfmt == BLAST_E4M3)
-    return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, false, 0, 0>(a, stream) : launch_linear8<B, DUAL, false, 0, 1>(a, stream);
-  return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, false, 1, 0>(a, stream) : launch_linear8<B, DUAL, false, 1, 1>(a, stream);
+    return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, EXACT, 0, 0>(a, stream) : launch_linear8<B, DUAL, EXACT, 0, 1>(a, stream);
+  return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, EXACT, 1, 0>(a, stream) : launch_linear8<B, DUAL, EXACT, 1, 1>(a, stream);
 }
 
 }  // namespace
@@ -122,8 +123,8 @@ extern "C" int blast_bsr_linear_scaled8(const blast_bsr_view* W, const blast_wei
   a.y_vec = blast::aligned(Y, 16) && ldy * (a.y_bf16 ? 2 : 4) % 16 == 0;
   if (Y8) a.y8 = eight_of(Y8);
   if (Z8) a.k8[0] = eight_of(Z8);
-  const bool exact = Y && !a.y_bf16;
-  return W->b == 64 ? by_formats<64, false>(a, exact, stream) : by_formats<128, false>(a, exact, stream);
+  if (Y && !a.y_bf16) return W->b == 64 ? by_formats<64, false, true>(a, stream) : by_formats<128, false, true>(a, stream);
+  return W->b == 64 ? by_formats<64, false, false>(a, stream) : by_formats<128, false, false>(a, stream);
 }
 
 extern "C" int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_weight8_view* gate8, const blast_bsr_view* Wup,
@@ -162,5 +163,5 @@ extern "C" int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_
   if (H8) a.y8 = eight_of(H8);
   if (G8) a.k8[0] = eight_of(G8);
   if (U8) a.k8[1] = eight_of(U8);
-  return Wgate->b == 64 ? by_formats<64, true>(a, false, stream) : by_formats<128, true>(a, false, stream);
+  return Wgate->b == 64 ? by_formats<64, true, false>(a, stream) : by_formats<128, true, false>(a, stream);
 }

@@ -104,20 +104,20 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi, int fmt, float scale) {
   return __builtin_bit_cast(bf16x8, (u32x4{a[0], a[1], b[0], b[1]}));
 }
 
-// 64 of the contraction on 32 x 32 tiles: a lane has 32 bytes of a row of each operand, the same places on both.  EXACT: widened;
-// else in formats WF, XF.
+// 64 of the contraction on 32 x 32 tiles: a lane has 32 bytes of a row of each operand, in formats WF and XF, the same places on both.
+// EXACT: widened to bf16 (the formats are constants for that too: a branch at every conversion kept conversions and matrix instructions
+// apart, 2048 x 8192 at 90 %, 2048 tokens, fp32 32.6 us, 21.2 without).
 template <int RT, int NT, bool EXACT, int WF, int XF>
-__device__ __forceinline__ void multiply8(f32x16 (&d)[RT][NT], const i32x8 (&fw)[RT], const i32x8 (&fx)[NT], int ws, const int (&xs)[NT],
-                                          int wfmt, int xfmt) {
+__device__ __forceinline__ void multiply8(f32x16 (&d)[RT][NT], const i32x8 (&fw)[RT], const i32x8 (&fx)[NT], int ws, const int (&xs)[NT]) {
   if constexpr (EXACT) {
     const float wsf = scale_value(ws);
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       bf16x8 bw[RT], bx[NT];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) bw[i] = widen8(fw[i][2 * p], fw[i][2 * p + 1], wfmt, wsf);
+      for (int i = 0; i < RT; ++i) bw[i] = widen8(fw[i][2 * p], fw[i][2 * p + 1], WF, wsf);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) bx[j] = widen8(fx[j][2 * p], fx[j][2 * p + 1], xfmt, scale_value(xs[j]));
+      for (int j = 0; j < NT; ++j) bx[j] = widen8(fx[j][2 * p], fx[j][2 * p + 1], XF, scale_value(xs[j]));
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256, B == 64 && !DUAL ? 3 : 2) void k_linear8(const
         fx[j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         xs[j] = sc[(KB == 2 ? kk : 0) * 256 + row];
       }
-      multiply8<2, NT, EXACT, WF, XF>(d, fw, fx, kk && KB == 2 ? w1 : w0, xs, a.wfmt, a.x.fmt);
+      multiply8<2, NT, EXACT, WF, XF>(d, fw, fx, kk && KB == 2 ? w1 : w0, xs);
     }
   };
 
@@ -712,7 +712,7 @@ __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
       fx[k][0] = __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
     }
 #pragma unroll
-    for (int k = 0; k < KS; ++k) multiply8<RT, 1, EXACT, WF, XF>(d, fw[k], fx[k], ws, xs, a.wfmt, a.x.fmt);
+    for (int k = 0; k < KS; ++k) multiply8<RT, 1, EXACT, WF, XF>(d, fw[k], fx[k], ws, xs);
   };
   // the blocks of both matrices are dealt as one sequence
 #pragma unroll 1
