@@ -5,7 +5,8 @@ Two kinds of block alternate, as the two MLPs of the paper's models:
   gated          y = Wdown (silu(Wgate x) * Wup x), normalised, gated per feature, scaled and added by norm_residual, which
                  also takes the norm that the next block reads.
 The gradient of every weight block is kept for the stored blocks only; G and U of the gated block are made again on the way
-back instead of being kept.  Run: python examples/train_block.py
+back instead of being kept.  With eight_bit=True a gated block multiplies in scaled 8-bit form in both directions, and what it keeps of
+a step - its input, G, U and H - stays in that form, a quarter of their bytes in 32 bits.  Run: python examples/train_block.py
 """
 import os
 import sys
@@ -37,6 +38,10 @@ class Weight:
     def __call__(self, x, **kw):
         return api.bsr_linear(self.packed, x, out_dtype=BF16, **kw)
 
+    def eight(self, transposed=False):
+        """The stored blocks as they are now, or those of the transpose, in 8 bits."""
+        return api.bsr_quantize_scaled8(api.bsr_transpose(self.packed) if transposed else self.packed)
+
     def backward(self, dy, x, dx_dtype=BF16):
         """(gradient of x, gradient of the stored blocks)."""
         return api.bsr_spmm(api.bsr_transpose(self.packed), dy, out_dtype=dx_dtype), api.bsr_sddmm(self.packed, dy, x)
@@ -47,9 +52,9 @@ class Weight:
 
 
 class Network:
-    def __init__(self, width=512, inter=2048, blocks=4, b=64, sparsity=0.8, seed=0):
+    def __init__(self, width=512, inter=2048, blocks=4, b=64, sparsity=0.8, seed=0, eight_bit=False):
         gen = torch.Generator(device="cuda").manual_seed(seed)
-        self.width = width
+        self.width, self.b, self.eight_bit = width, b, eight_bit
         ones, zeros = (lambda n: torch.ones(n, device="cuda")), (lambda n: torch.zeros(n, device="cuda"))
         self.blocks = []
         for k in range(blocks):
@@ -83,6 +88,12 @@ class Network:
                 h = api.bsr_linear(blk["w2"].packed, a, bias=blk["b2"], residual=h)  # fp32, a new stream: the old one is kept
                 _, x, stats = api.norm_residual(h, with_stats=True, **self._norm(blk))
                 saved = (x_in, z, a, h, None, stats)
+            elif self.eight_bit:
+                x_in = api.quantize_scaled8(x, group=self.b)
+                inner = api.bsr_gated_scaled8(blk["gate"].eight(), blk["up"].eight(), x_in, keep=keep is not None)
+                y = api.bsr_linear_scaled8(blk["down"].eight(), inner.H, out_dtype=BF16)
+                h, x, stats = api.norm_residual(h, y, with_stats=True, **self._norm(blk))
+                saved = (x_in, inner, None, h, y, stats)
             else:
                 y = api.sparse_mlp(blk["gate"].packed, blk["up"].packed, blk["down"].packed, x, out_dtype=BF16)
                 h, x, stats = api.norm_residual(h, y, with_stats=True, **self._norm(blk))
@@ -104,6 +115,20 @@ class Network:
                 through = api.act_backward(z, da, act="gelu", bias_grad=True)
                 dx, dw1 = blk["w1"].backward(through.dZ, x)
                 grads.append({"w1": dw1, "w2": dw2, "b1": through.dbias, "b2": into.dbias, "weight": g.dweight, "bias": g.dbias})
+            elif self.eight_bit:
+                dy, inner = g.dy, z
+
+                def eight(t):  # a gradient as an operand: more range, fewer digits
+                    return api.quantize_scaled8(t, group=self.b, fmt="e5m2")
+
+                dact = api.bsr_linear_scaled8(blk["down"].eight(True), eight(dy), out_dtype=BF16)
+                through = api.gated_act_backward_scaled8(inner.G, inner.U, dact, with_h=False)
+                dx_gate = api.bsr_linear_scaled8(blk["gate"].eight(True), eight(through.dG))
+                dx = api.bsr_linear_scaled8(blk["up"].eight(True), eight(through.dU), residual=dx_gate, out_dtype=BF16)
+                grads.append({"gate": api.bsr_sddmm_scaled8(blk["gate"].packed, through.dG, x),
+                              "up": api.bsr_sddmm_scaled8(blk["up"].packed, through.dU, x),
+                              "down": api.bsr_sddmm_scaled8(blk["down"].packed, dy, inner.H), "weight": g.dweight,
+                              "post_weight": g.dpost_weight, "scale_gate": g.dgate})
             else:
                 gate, up = blk["gate"](x), blk["up"](x)
                 dy = g.dy
@@ -170,6 +195,8 @@ def train(net, steps=30, tokens=512, rate=0.02, seed=1):
 
 
 def main():
+    losses = train(Network(eight_bit=True))
+    print("gated blocks in 8 bits: loss %.4f -> %.4f" % (losses[0], losses[-1]))
     net = Network()
     losses = train(net)
     print("loss %.4f -> %.4f" % (losses[0], losses[-1]))

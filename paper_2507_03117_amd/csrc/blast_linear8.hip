@@ -3,7 +3,6 @@
 
 #include "kern_linear8.h"
 
-
 using namespace blast_dev;
 
 namespace {
@@ -34,14 +33,23 @@ int check_out8(const blast_scaled8_view* v, const blast_bsr_view* W, int64_t T) 
   return check_eight(v, T, W->rows, 16);
 }
 
-// Workgroups for tiles of TT tokens.  Many tiles: two XCDs share a block row, each with half of its tokens (53248 x 16384 at 95 %, 2048
-// tokens, one / two / four / eight XCDs to a row: 148 / 142 / 149 / 154 us; gated 14336 x 4096, 4096 tokens 85 / 84 / 85 / 84).  An odd
-// number of tiles leaves one of two XCDs a tile short.
-int64_t grid8(Linear8Args& a, int TT) {
+int cu_count8() {
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 256;
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) return 256;
+  return n;
+}
+
+// Workgroups for tiles of TT tokens: one for each, or as many as are resident at once; 0: more tiles than can be counted.  Many tiles: two
+// XCDs share a block row, each with half of its tokens (53248 x 16384 at 95 %, 2048 tokens, one / two / four / eight XCDs to a row: 148 /
+// 142 / 149 / 154 us; gated 14336 x 4096, 4096 tokens 85 / 84 / 85 / 84).  An odd number of tiles leaves one of two XCDs a tile short.
+int64_t grid8(Linear8Args& a, int TT, int64_t resident) {
   a.ntt = (int)(((int64_t)a.T + TT - 1) / TT);
   a.parts = TT >= 128 && a.ntt >= 2 && (a.ntt % 2 == 0 || a.ntt >= 16) ? 2 : 1;
   const int64_t rows = 8 / a.parts;
-  return 8 * (((int64_t)a.nbr + rows - 1) / rows) * (((int64_t)a.ntt + a.parts - 1) / a.parts);
+  const int64_t most = (((int64_t)a.nbr + rows - 1) / rows) * (((int64_t)a.ntt + a.parts - 1) / a.parts);  // of an XCD
+  if (most > INT32_MAX / 8) return 0;
+  return 8 * (most < resident / 8 ? most : resident / 8 < 1 ? 1 : resident / 8);
 }
 
 template <class K>
@@ -62,16 +70,16 @@ int launch_linear8(Linear8Args a, hipStream_t stream) {
   if (a.T <= 32 || tiles < kFewTiles) {
     using C = S8Cfg<B, DUAL>;
     if (int rc = raise_lds(&k_linear8_split<B, DUAL, EXACT, WF, XF>, C::LDS_BYTES, split_set)) return rc;
-    const int64_t grid = grid8(a, C::TT);
-    if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
+    const int64_t grid = grid8(a, C::TT, INT32_MAX);
+    if (grid == 0) return BLAST_ERR_INVALID_ARG;
     k_linear8_split<B, DUAL, EXACT, WF, XF><<<dim3((unsigned)grid), dim3(64 * C::NW), C::LDS_BYTES, stream>>>(a);
     BLAST_LAUNCH_CHECK("k_linear8_split");
     return BLAST_OK;
   }
   using C = L8Cfg<B>;
   if (int rc = raise_lds(&k_linear8<B, DUAL, EXACT, WF, XF>, C::LDS_BYTES, tile_set)) return rc;
-  const int64_t grid = grid8(a, C::TT);
-  if (grid > INT32_MAX) return BLAST_ERR_INVALID_ARG;
+  const int64_t grid = grid8(a, C::TT, 2 * cu_count8());
+  if (grid == 0) return BLAST_ERR_INVALID_ARG;
   k_linear8<B, DUAL, EXACT, WF, XF><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a);
   BLAST_LAUNCH_CHECK("k_linear8");
   return BLAST_OK;

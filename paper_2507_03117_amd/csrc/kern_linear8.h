@@ -2,9 +2,15 @@
 // residual, or the gated pair; results in fp32, bf16 or scaled 8-bit form.  Features are the M dimension of the matrix instruction,
 // tokens the N dimension: a lane has one token and hands over its scale with the codes.
 //
-// k_linear8: a workgroup of four waves has a block row's B rows of 128 tokens.  A step is 128 of the contraction: a stored block of
-// 128 x 128 or two of 64 x 64, W and X tiles copied to LDS in rows of 128 bytes, the scales of the step's tokens beside them; the next
-// step's copies are under way while one is multiplied.
+// k_linear8: workgroups of four waves, two on a CU, walk lists of tiles: a block row's B rows of 128 tokens.  A step is 128 of the
+// contraction: a stored block of 128 x 128 or two of 64 x 64, W and X tiles copied to LDS in rows of 128 bytes, the scales of the step's
+// tokens beside them; the next step's copies are under way while one is multiplied, the next tile's first step while a tile's results
+// leave (53248 x 16384 at 95 %, 2048 tokens, a workgroup for each tile 148 us, lists 142; gated 14336 x 4096, 4096 tokens, 84 / 82).
+//
+// Bound, 53248 x 16384 at 95 %, 2048 tokens, bf16: bytes from beyond the L2s - a row's few blocks need other activations than the
+// next row's, so that a byte of X is fetched for every block that reads it (0.7 GB), 0.96 GB with W and the result at 6.8 TB/s; the matrix cores
+// are busy a quarter of the time.  Gated 14336 x 4096 at 95 %, 4096 tokens, G, U and H kept in 8 bits: the 176 MB of results (20 us for G and
+// U, 7 for SiLU) on top of 42 us of steps, which a row of 1.6 blocks a matrix keeps short.
 // k_linear8_split: eight waves have a block row's B rows of 32 tokens and deal the stored blocks among themselves, operands straight
 // into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
 #pragma once
@@ -132,26 +138,20 @@ __device__ __forceinline__ void multiply8(f32x16 (&d)[RT][NT], const i32x8 (&fw)
   }
 }
 
-// Workgroup ids go round the eight XCDs.  Each has every (8 / parts)th block row and one of `parts` runs of the token tiles, a row's tiles
-// one after the other.
-__device__ __forceinline__ bool place8(const Linear8Args& a, int& rank, int& tt) {
-  const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3, per = (a.ntt + a.parts - 1) / a.parts;
+// The tiles (block row, run of tokens) in eight lists, one for each XCD: an XCD has every (8 / parts)th block row and one of `parts`
+// runs of the token tiles, a row's tiles one after the other.  Workgroup ids go round the XCDs; the workgroups of an XCD deal its list.
+__device__ __forceinline__ bool place8(const Linear8Args& a, int item, int& rank, int& tt) {
+  const int xcd = blockIdx.x & 7, per = (a.ntt + a.parts - 1) / a.parts, k = ((int)blockIdx.x >> 3) + item * ((int)gridDim.x >> 3);
   rank = k / per * (8 / a.parts) + xcd / a.parts;
   tt = xcd % a.parts * per + k % per;
   return rank < a.nbr && tt < a.ntt;
 }
-
-// Columns and scales of a block row's stored blocks, one a lane, 64 at a time.
-struct Blocks8 {
-  int col, scale;
-  __device__ __forceinline__ void load(const Mat8& m, int first, int n, int lane) {
-    col = scale = 0;
-    if (lane < n) {
-      col = m.col_idx[first + lane];
-      scale = m.scales[first + lane];
-    }
-  }
-};
+// How many of them this workgroup has.
+__device__ __forceinline__ int items8(const Linear8Args& a) {
+  const int xcd = blockIdx.x & 7, per = (a.ntt + a.parts - 1) / a.parts, rows = 8 / a.parts, mine = xcd / a.parts;
+  const int n = (a.nbr > mine ? (a.nbr - mine + rows - 1) / rows : 0) * per, step = (int)gridDim.x >> 3, first = (int)blockIdx.x >> 3;
+  return n > first ? (n - first + step - 1) / step : 0;
+}
 
 template <int B>
 struct L8Cfg {
@@ -164,13 +164,14 @@ struct L8Cfg {
   static constexpr int NT = TW / 32;
   static constexpr int W_BYTES = B * 128, X_BYTES = TT * 128;
   static constexpr int WI = W_BYTES / (1024 * NW), XI = X_BYTES / (1024 * NW);  // copy instructions of a wave, 1 KiB each
+  static constexpr int OPS = WI + XI + 1;       // with the one of the tokens' scales
   static constexpr int S_BYTES = KB * 256;
   static constexpr int STAGE = W_BYTES + X_BYTES + S_BYTES;
   static constexpr int RING = NSTAGE * STAGE;
   static constexpr int EX_BYTES = 3 * WR * TT * 4;  // largest magnitudes that the waves of a token's rows tell each other
   static constexpr int LDS_BYTES = RING + EX_BYTES;
   static constexpr int OUT_BYTES = 4096;            // a wave's part of a stage when results leave
-  static_assert(2 * B * TT + NW * OUT_BYTES <= RING && 3 * B * TT <= RING && LDS_BYTES <= 160 * 1024, "");
+  static_assert(2 * B * TT <= STAGE && NW * OUT_BYTES <= STAGE && LDS_BYTES <= 160 * 1024, "");
 };
 
 // ---- results: a wave's 64 rows of 32 NT tokens, as the matrix instruction leaves them ----------------------------------------------
@@ -293,12 +294,12 @@ __device__ __forceinline__ void put_eight(const Eight& o, const f32x16 (&d)[2][N
 }
 // The tile's codes out of LDS, by all threads.
 template <int B, int TT>
-__device__ __forceinline__ void leave_eight(const Eight& o, const unsigned char* lds, int64_t t0, int64_t T, int64_t row0) {
+__device__ __forceinline__ void leave_eight(const Eight& o, const unsigned char* lds, int thread, int64_t t0, int64_t T, int64_t row0) {
   constexpr int kLanes = B / 16, kTokens = 256 / kLanes;
-  const int c = threadIdx.x % kLanes;
+  const int c = thread % kLanes;
 #pragma unroll
   for (int k = 0; k < TT / kTokens; ++k) {
-    const int tok = k * kTokens + threadIdx.x / kLanes;
+    const int tok = k * kTokens + thread / kLanes;
     const u32x4 w = *reinterpret_cast<const u32x4*>(lds + code_at<B>(tok, c));
     if (t0 + tok < T) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(o.codes + (t0 + tok) * o.ld + row0 + 16 * c));
   }
@@ -416,28 +417,41 @@ __device__ __forceinline__ void put_sums(const Linear8Args& a, const f32x16 (&d)
   }
 }
 
+// What a workgroup has to do, one item a lane: block row, first token, first stored block and number of stored blocks of each matrix.
+template <int NM, int TT>
+struct Items8 {
+  int row, t0, kb[NM], nb[NM];
+  __device__ __forceinline__ void load(const Linear8Args& a, int first, int n, int lane) {
+    row = t0 = 0;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) kb[m] = nb[m] = 0;
+    if (first + lane < n) {
+      int rank, tt;
+      const bool there = place8(a, first + lane, rank, tt);
+      t0 = a.T;  // (a place beyond the last tile: no blocks, no token)
+      if (there) {
+        row = a.row_order ? a.row_order[rank] : rank;
+        t0 = tt * TT;
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+          kb[m] = a.m[m].row_ptr[row];
+          nb[m] = a.m[m].row_ptr[row + 1] - kb[m];
+        }
+      }
+    }
+  }
+};
+
 template <int B, bool DUAL, bool EXACT, int WF, int XF>
-__global__ __launch_bounds__(256, B == 64 && !DUAL ? 3 : 2) void k_linear8(const Linear8Args a) {
+__global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
   using C = L8Cfg<B>;
-  constexpr int NW = C::NW, NT = C::NT, KB = C::KB, NM = DUAL ? 2 : 1, TT = C::TT;
+  constexpr int NW = C::NW, NSTAGE = C::NSTAGE, NT = C::NT, KB = C::KB, NM = DUAL ? 2 : 1, TT = C::TT;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l32 = lane & 31, lh = lane >> 5;
   const int wr = wave / C::WT, wt = wave % C::WT;  // this wave's 64 rows and TW tokens
-  int rank, tt;
-  if (!place8(a, rank, tt)) return;
-  const int r = a.row_order ? ld_idx(a.row_order, rank) : rank, t0 = tt * TT;
-  int kb[NM], nb[NM], steps[NM];
-  Blocks8 blocks[NM];
-#pragma unroll
-  for (int m = 0; m < NM; ++m) {
-    kb[m] = ld_idx(a.m[m].row_ptr, r);
-    nb[m] = ld_idx(a.m[m].row_ptr, r + 1) - kb[m];
-    steps[m] = (nb[m] + KB - 1) / KB;
-  }
-#pragma unroll
-  for (int m = 0; m < NM; ++m) blocks[m].load(a.m[m], kb[m], nb[m], lane);
-  const int total = steps[0] + (DUAL ? steps[NM - 1] : 0);
+  const int n_items = items8(a);
+  if (n_items <= 0) return;
 
   // Copy side: position p (16 bytes) of a tile = row p / 8, slot p % 8; it holds chunk slot ^ row % 8 of that row's 128 bytes, which for
   // two blocks are 64 of each.  (row % 8 = lane / 8: a lane's chunk is the same in every instruction.)
@@ -447,47 +461,65 @@ __global__ __launch_bounds__(256, B == 64 && !DUAL ? 3 : 2) void k_linear8(const
   uint32_t woff[C::WI];
 #pragma unroll
   for (int i = 0; i < C::WI; ++i) woff[i] = (uint32_t)(((i * NW + wave) * 8 + (lane >> 3)) * B) + coff;
-  const uint8_t* xrow[C::XI];
-#pragma unroll
-  for (int i = 0; i < C::XI; ++i) {
-    int t = t0 + (i * NW + wave) * 8 + (lane >> 3);
-    t = t < a.T ? t : a.T - 1;  // rows beyond the last token read it again; nothing of them is stored
-    xrow[i] = a.x.codes + t * a.x.ld + coff;
-  }
-  int64_t soff = t0 + 4 * (lane < TT / 4 ? lane : TT / 4 - 1);
-  soff = soff < a.x.lds - 4 ? soff : a.x.lds - 4;
 
-  auto issue = [&](int m, int s, int slot) {
-    unsigned char* st = smem + slot * C::STAGE;
-    const int b0 = s * KB;
-    if (b0 > 0 && (b0 & 63) == 0) blocks[m].load(a.m[m], kb[m] + b0, nb[m] - b0, lane);
-    const bool two = KB == 2 && b0 + 1 < nb[m];
-    const int c0 = __builtin_amdgcn_readlane(blocks[m].col, b0 & 63);
-    const int c1 = two ? __builtin_amdgcn_readlane(blocks[m].col, (b0 + 1) & 63) : c0;
-    const int q0 = kb[m] + b0, q1 = two ? q0 + 1 : q0;
-    const uint8_t* wsrc = a.m[m].vals + (int64_t)(second ? q1 : q0) * (B * B);
-    const int64_t xcol = (int64_t)(second ? c1 : c0) * B;
+  // The loader runs NSTAGE - 1 steps ahead of the multiplier, over the same sequence of items, matrices and steps.
+  Items8<NM, TT> batch;
+  int l_item = -1, l_m = NM - 1, l_s = 0, l_kb = 0, l_nb = 0, l_t0 = 0, l_c0 = 0, l_c1 = 0, l_slot = 0, ahead = 0;
+  bool l_valid = true;
+  const uint8_t* xrow[C::XI];
+  int64_t soff = 0;
+  auto seek = [&]() {  // to the next step that there is
+    while (l_s * KB >= l_nb) {
+      l_s = 0;
+      if (++l_m < NM) {
+        l_kb = __builtin_amdgcn_readlane(batch.kb[NM - 1], l_item & 63);
+        l_nb = __builtin_amdgcn_readlane(batch.nb[NM - 1], l_item & 63);
+        continue;
+      }
+      l_m = 0;
+      if (++l_item >= n_items) {
+        l_valid = false;
+        return;
+      }
+      if ((l_item & 63) == 0) batch.load(a, l_item, n_items, lane);
+      l_kb = __builtin_amdgcn_readlane(batch.kb[0], l_item & 63);
+      l_nb = __builtin_amdgcn_readlane(batch.nb[0], l_item & 63);
+      l_t0 = __builtin_amdgcn_readlane(batch.t0, l_item & 63);
+#pragma unroll
+      for (int i = 0; i < C::XI; ++i) {
+        int t = l_t0 + (i * NW + wave) * 8 + (lane >> 3);
+        t = t < a.T ? t : a.T - 1;  // rows beyond the last token read it again; nothing of them is stored
+        xrow[i] = a.x.codes + t * a.x.ld + coff;
+      }
+      soff = l_t0 + 4 * (lane < TT / 4 ? lane : TT / 4 - 1);
+      soff = soff < a.x.lds - 4 ? soff : a.x.lds - 4;
+    }
+    const Mat8& m = a.m[DUAL ? l_m : 0];
+    l_c0 = ld_idx(m.col_idx, l_kb + l_s * KB);
+    l_c1 = KB == 2 && l_s * KB + 1 < l_nb ? ld_idx(m.col_idx, l_kb + l_s * KB + 1) : l_c0;
+  };
+  auto issue = [&]() {
+    unsigned char* st = smem + l_slot * C::STAGE;
+    const Mat8& m = a.m[DUAL ? l_m : 0];
+    const int q0 = l_kb + l_s * KB, q1 = KB == 2 && l_s * KB + 1 < l_nb ? q0 + 1 : q0;
+    const uint8_t* wsrc = m.vals + (int64_t)(second ? q1 : q0) * (B * B);
+    const int64_t xcol = (int64_t)(second ? l_c1 : l_c0) * B;
 #pragma unroll
     for (int i = 0; i < C::WI; ++i) BLAST_GLDS16(wsrc + woff[i], st + (i * NW + wave) * 1024);
 #pragma unroll
     for (int i = 0; i < C::XI; ++i) BLAST_GLDS16(xrow[i] + xcol, st + C::W_BYTES + (i * NW + wave) * 1024);
     // (every wave copies the scales of one of the step's blocks: those that copy the same write the same)
-    const int which = wave % KB, cs = which ? c1 : c0;
+    const int which = wave % KB, cs = which ? l_c1 : l_c0;
     __builtin_amdgcn_global_load_lds(
         (const __attribute__((address_space(1))) void*)(a.x.scales + (((int64_t)cs * B) >> a.x.shift) * a.x.lds + soff),
         (__attribute__((address_space(3))) void*)(st + C::W_BYTES + C::X_BYTES + which * 256), 4, 0, 0);
+    l_slot = l_slot + 1 == NSTAGE ? 0 : l_slot + 1;
+    ++ahead;
+    ++l_s;
+    seek();
   };
 
   f32x16 acc[NM][2][NT];
-#pragma unroll
-  for (int m = 0; m < NM; ++m)
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[m][i][j][v] = 0.0f;
-
   // Fragment side: of each 64 of a row lane half h takes chunks h and h + 2, the same on both operands.
   auto chunk_at = [&](int row, int c) { return (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4)); };
   auto multiply = [&](f32x16 (&d)[2][NT], int w0, int w1, bool two, int slot) {
@@ -517,142 +549,175 @@ __global__ __launch_bounds__(256, B == 64 && !DUAL ? 3 : 2) void k_linear8(const
     }
   };
 
-  // The two matrices' steps are one sequence; what a step multiplies by is read from its blocks' lanes before the next one is issued.
-  auto issue_step = [&](int g) {
-    if (!DUAL || g < steps[0])
-      issue(0, g, g & 1);
-    else
-      issue(NM - 1, g - steps[0], g & 1);
+  int slot = 0;  // of the step multiplied next
+  auto meet = [&]() {  // all waves' LDS accesses so far; no copy is waited for
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
-  auto run = [&](int m, f32x16 (&d)[2][NT], int base) {
+  auto run = [&](f32x16 (&d)[2][NT], const Mat8& m, int kb, int nb) {
 #pragma unroll 1
-    for (int s = 0; s < steps[m]; ++s) {
-      const int g = base + s, b0 = s * KB;
-      const bool two = KB == 2 && b0 + 1 < nb[m];
-      const int w0 = __builtin_amdgcn_readlane(blocks[m].scale, b0 & 63), w1 = __builtin_amdgcn_readlane(blocks[m].scale, (b0 + 1) & 63);
-      __builtin_amdgcn_s_waitcnt(BLAST_VMCNT(0));  // this wave's copies of the step have landed (a barrier need not wait for a copy)
-      __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): what was read of the step before is here
+    for (int b0 = 0; b0 < nb; b0 += KB) {
+      const int q = kb + b0;
+      const bool two = KB == 2 && b0 + 1 < nb;
+      const int w0 = (ld_idx(reinterpret_cast<const int*>(m.scales), q >> 2) >> (8 * (q & 3))) & 255;
+      const int w1 = two ? (ld_idx(reinterpret_cast<const int*>(m.scales), (q + 1) >> 2) >> (8 * ((q + 1) & 3))) & 255 : w0;
+      // Copies retire in the order in which they were asked for: all but those of the steps after this one.  (__syncthreads would wait for
+      // those too.)
+      if (NSTAGE > 2 && ahead == NSTAGE - 1)
+        __builtin_amdgcn_s_waitcnt(BLAST_VMCNT((NSTAGE - 2) * C::OPS));
+      else
+        __builtin_amdgcn_s_waitcnt(BLAST_VMCNT(0));
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): what was read of the step before is here
       asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_barrier();  // so have everybody's, and the stage of the step before is free
+      __builtin_amdgcn_s_barrier();  // everybody's copies of this step have landed, and the stage of the step before is free
       asm volatile("" ::: "memory");
-      if (g + 1 < total) issue_step(g + 1);
-      multiply(d, w0, w1, two, g & 1);
+      --ahead;
+      if (l_valid) issue();
+      multiply(d, w0, w1, two, slot);
+      slot = slot + 1 == NSTAGE ? 0 : slot + 1;
     }
   };
-  if (total > 0) issue_step(0);
-  run(0, acc[0], 0);
-  if constexpr (DUAL) run(1, acc[NM - 1], steps[0]);
 
-  // Results, by way of the ring, whose last step a barrier below has seen read.  `ex`: largest magnitudes over a wave's rows of each
-  // token, of up to three tensors; a group of 128 rows is two waves'.
-  unsigned char* lds = smem + 2 * B * TT + wave * C::OUT_BYTES;  // (behind the codes of two tensors)
-  uint32_t* ex = reinterpret_cast<uint32_t*>(smem + C::RING);
-  const int64_t tw = t0 + wt * C::TW, row0 = (int64_t)r * B + wr * 64;
-  auto tell = [&](int k, const uint32_t (&m)[NT]) {
-    if (lh == 0) {
+  seek();
+#pragma unroll 1
+  for (int g = 0; g < NSTAGE - 1; ++g)
+    if (l_valid) issue();
+
+  Items8<NM, TT> mine;
+#pragma unroll 1
+  for (int item = 0; item < n_items; ++item) {
+    if ((item & 63) == 0) mine.load(a, item, n_items, lane);
+    const int r = __builtin_amdgcn_readlane(mine.row, item & 63), t0 = __builtin_amdgcn_readlane(mine.t0, item & 63);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) ex[(k * C::WR + wr) * TT + wt * C::TW + 32 * j + l32] = m[j];
+    for (int m = 0; m < NM; ++m) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[m][i][j][v] = 0.0f;
+      run(acc[m], a.m[m], __builtin_amdgcn_readlane(mine.kb[m], item & 63), __builtin_amdgcn_readlane(mine.nb[m], item & 63));
     }
-  };
-  auto told = [&](int k, uint32_t (&m)[NT]) {
+
+    // Results, by way of the stage that no copy is on its way to.  `ex`: largest magnitudes over a wave's rows of each token, of up to
+    // three tensors; a group of 128 rows is two waves'.
+    int ln = lane;
+    asm volatile("" : "+v"(ln));  // (what follows from it is made here again, not kept in registers through the steps)
+    const int l32 = ln & 31, lh = ln >> 5, thread = wave * 64 + ln;
+    unsigned char* stage = smem + (slot == 0 ? NSTAGE - 1 : slot - 1) * C::STAGE;
+    unsigned char* lds = stage + wave * C::OUT_BYTES;
+    uint32_t* ex = reinterpret_cast<uint32_t*>(smem + C::RING);
+    const int64_t tw = t0 + wt * C::TW, row0 = (int64_t)r * B + wr * 64;
+    auto tell = [&](int k, const uint32_t (&m)[NT]) {
+      if (lh == 0) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      m[j] = 0;
-#pragma unroll
-      for (int w = 0; w < C::WR; ++w) {
-        const uint32_t o = ex[(k * C::WR + w) * TT + wt * C::TW + 32 * j + l32];
-        m[j] = o > m[j] ? o : m[j];
+        for (int j = 0; j < NT; ++j) ex[(k * C::WR + wr) * TT + wt * C::TW + 32 * j + l32] = m[j];
       }
-    }
-  };
-  constexpr int kCodes = B * TT;  // bytes of the tile's codes
-  const int tok0 = wt * C::TW;
-  const int64_t rows0 = (int64_t)r * B;
-  if constexpr (DUAL) {
-    const bool keep_g = a.k8[0].codes, keep_u = a.k8[1].codes, to8 = a.y8.codes;
-    uint32_t m[NT];
-    if (keep_g) token_max<NT>(acc[0], m), tell(0, m);
-    if (keep_u) token_max<NT>(acc[1], m), tell(1, m);
-    __syncthreads();  // (everybody has read the last step; what was told can be heard)
-    if (keep_g) told(0, m), put_eight<B, NT>(a.k8[0], acc[0], m, smem, lane, tok0, wr * 64, t0, a.T, r);
-    if (keep_u) told(1, m), put_eight<B, NT>(a.k8[1], acc[1], m, smem + kCodes, lane, tok0, wr * 64, t0, a.T, r);
-    f32x16 (&h)[2][NT] = acc[0];
-    with_act(a.act, [&](auto act) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) h[i][j][v] = act_of(act, h[i][j][v]) * acc[1][i][j][v];
-    });
-    if (to8) token_max<NT>(h, m), tell(2, m);
-    __syncthreads();  // (G's and U's codes are in LDS)
-    if (keep_g) leave_eight<B, TT>(a.k8[0], smem, t0, a.T, rows0);
-    if (keep_u) leave_eight<B, TT>(a.k8[1], smem + kCodes, t0, a.T, rows0);
-    if (to8) {
-      told(2, m), put_eight<B, NT>(a.y8, h, m, smem + 2 * kCodes, lane, tok0, wr * 64, t0, a.T, r);
-      __syncthreads();
-      leave_eight<B, TT>(a.y8, smem + 2 * kCodes, t0, a.T, rows0);
-    } else {
-      put_bf16<NT>(static_cast<uint16_t*>(a.y), a.ldy, a.y_vec, h, lds, lane, tw, a.T, row0);
-    }
-  } else {
-    f32x16 (&d)[2][NT] = acc[0];
-    if (a.bias) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const float b = a.bias[row0 + 32 * i + 8 * (v >> 2) + 4 * lh + (v & 3)];
-#pragma unroll
-          for (int j = 0; j < NT; ++j) d[i][j][v] += b;
-        }
-    }
-    const bool keep = a.k8[0].codes, to8 = a.y8.codes;
-    uint32_t m[NT];
-    if (keep) token_max<NT>(d, m), tell(0, m);
-    __syncthreads();  // (everybody has read the last step; what was told can be heard)
-    if (keep) {
-      told(0, m), put_eight<B, NT>(a.k8[0], d, m, smem, lane, tok0, wr * 64, t0, a.T, r);
-      __syncthreads();
-      leave_eight<B, TT>(a.k8[0], smem, t0, a.T, rows0);
-    }
-    with_act(a.act, [&](auto act) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) d[i][j][v] = act_of(act, d[i][j][v]);
-    });
-    const bool added = to8 && a.r;  // (before the result is written: it may be where the residual is)
-    if (added) {
+    };
+    auto told = [&](int k, uint32_t (&m)[NT]) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        const int64_t t = tw + 32 * j + l32;
+        m[j] = 0;
+#pragma unroll
+        for (int w = 0; w < C::WR; ++w) {
+          const uint32_t o = ex[(k * C::WR + w) * TT + wt * C::TW + 32 * j + l32];
+          m[j] = o > m[j] ? o : m[j];
+        }
+      }
+    };
+    constexpr int kCodes = B * TT;  // bytes of the tile's codes
+    const int tok0 = wt * C::TW;
+    const int64_t rows0 = (int64_t)r * B;
+    if constexpr (DUAL) {
+      const bool keep_g = a.k8[0].codes, keep_u = a.k8[1].codes, to8 = a.y8.codes;
+      uint32_t m[NT];
+      if (keep_g) token_max<NT>(acc[0], m), tell(0, m);
+      if (keep_u) token_max<NT>(acc[1], m), tell(1, m);
+      meet();  // (everybody has read the last step; what was told can be heard)
+      if (keep_g) told(0, m), put_eight<B, NT>(a.k8[0], acc[0], m, stage, ln, tok0, wr * 64, t0, a.T, r);
+      if (keep_u) told(1, m), put_eight<B, NT>(a.k8[1], acc[1], m, stage + kCodes, ln, tok0, wr * 64, t0, a.T, r);
+      f32x16 (&h)[2][NT] = acc[0];
+      with_act(a.act, [&](auto act) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int v = 0; v < 16; v += 4) {
-            float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (t < a.T) residual4(a, t, row0 + 32 * i + 2 * v + 4 * lh, q);
+          for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[i][j][v + e] += q[e];
+            for (int v = 0; v < 16; ++v) h[i][j][v] = act_of(act, h[i][j][v]) * acc[1][i][j][v];
+      });
+      if (to8) token_max<NT>(h, m), tell(2, m);
+      meet();  // (G's and U's codes are in LDS)
+      if (keep_g) leave_eight<B, TT>(a.k8[0], stage, thread, t0, a.T, rows0);
+      if (keep_u) leave_eight<B, TT>(a.k8[1], stage + kCodes, thread, t0, a.T, rows0);
+      meet();  // (and out of it)
+      if (to8) {
+        told(2, m), put_eight<B, NT>(a.y8, h, m, stage, ln, tok0, wr * 64, t0, a.T, r);
+        meet();
+        leave_eight<B, TT>(a.y8, stage, thread, t0, a.T, rows0);
+      } else {
+        put_bf16<NT>(static_cast<uint16_t*>(a.y), a.ldy, a.y_vec, h, lds, ln, tw, a.T, row0);
+      }
+    } else {
+      f32x16 (&d)[2][NT] = acc[0];
+      if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const float b = a.bias[row0 + 32 * i + 8 * (v >> 2) + 4 * lh + (v & 3)];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) d[i][j][v] += b;
           }
       }
-    }
-    if (a.y) {
-      if (!a.y_bf16 || (a.r && !added))
-        put_sums<NT>(a, d, a.r && !added, lds, lane, tw, row0);
-      else
-        put_bf16<NT>(static_cast<uint16_t*>(a.y), a.ldy, a.y_vec, d, lds, lane, tw, a.T, row0);
-    }
-    if (to8) {
-      token_max<NT>(d, m), tell(1, m);
-      __syncthreads();
-      told(1, m), put_eight<B, NT>(a.y8, d, m, smem + kCodes, lane, tok0, wr * 64, t0, a.T, r);
-      __syncthreads();
-      leave_eight<B, TT>(a.y8, smem + kCodes, t0, a.T, rows0);
+      const bool keep = a.k8[0].codes, to8 = a.y8.codes;
+      uint32_t m[NT];
+      if (keep) token_max<NT>(d, m), tell(0, m);
+      meet();  // (everybody has read the last step; what was told can be heard)
+      if (keep) {
+        told(0, m), put_eight<B, NT>(a.k8[0], d, m, stage, ln, tok0, wr * 64, t0, a.T, r);
+        meet();
+        leave_eight<B, TT>(a.k8[0], stage, thread, t0, a.T, rows0);
+        meet();
+      }
+      with_act(a.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) d[i][j][v] = act_of(act, d[i][j][v]);
+      });
+      const bool added = to8 && a.r;  // (before the result is written: it may be where the residual is)
+      if (added) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const int64_t t = tw + 32 * j + l32;
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4) {
+              float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+              if (t < a.T) residual4(a, t, row0 + 32 * i + 2 * v + 4 * lh, q);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) d[i][j][v + e] += q[e];
+            }
+        }
+      }
+      if (a.y) {
+        if (!a.y_bf16 || (a.r && !added))
+          put_sums<NT>(a, d, a.r && !added, lds, ln, tw, row0);
+        else
+          put_bf16<NT>(static_cast<uint16_t*>(a.y), a.ldy, a.y_vec, d, lds, ln, tw, a.T, row0);
+      }
+      if (to8) {
+        token_max<NT>(d, m), tell(1, m);
+        meet();
+        told(1, m), put_eight<B, NT>(a.y8, d, m, stage, ln, tok0, wr * 64, t0, a.T, r);
+        meet();
+        leave_eight<B, TT>(a.y8, stage, thread, t0, a.T, rows0);
+      }
     }
   }
 }
@@ -674,7 +739,7 @@ __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l32 = lane & 31, lh = lane >> 5;
   int rank, tt;
-  if (!place8(a, rank, tt)) return;
+  if (!place8(a, 0, rank, tt)) return;
   const int r = a.row_order ? ld_idx(a.row_order, rank) : rank;
   const int t0 = tt * C::TT;
   int kb[NM], nb[NM];

@@ -185,3 +185,8 @@ def test_reference_exponent_by_brute_force():
             want = next(e for e in range(-100, 130) if m <= ref.FORMATS[fmt][2] * 2.0 ** e)
             assert ref.exponent(m, fmt) == want and ref.exponents(np.array([m]), fmt)[0] == want
         assert ref.exponents(np.array([0.0]), fmt)[0] == -100
+
+
+def test_reference_codes_by_hand():
+    v = np.array([[0.0, 1.0, -1.0, 448.0], [464.0, -0.001, 0.0009765625, 0.00146484375]])
+    assert ref.encode(v.clip(-448, 448), "e4m3").tolist() == [[0, 0x38, 0xB8, 0x7E], [0x7E, 0x81, 0, 1]]
