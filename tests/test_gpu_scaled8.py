@@ -1,7 +1,7 @@
 """Operators on scaled 8-bit activations and weights against their definition in 64 bits.
 
 Tolerances.  Codes and scales of the quantisers are equal.  A sum that the 16-bit matrix instruction makes of the widened codes is off by at
-most n 2^-24 sum |products|, n the number of its terms.  The 8-bit instruction keeps of every product at least 15 bits below the
+most n 2^-24 sum |products|, n the number of its terms (fp32 and 8-bit results).  The 8-bit instruction (bf16 results alone) keeps of every product at least 15 bits below the
 largest of the 64 it adds at a time: 64 2^-15 of that largest one for each 64 terms, whose largest product is at most the
 largest weight times the largest activation among them.  What is stored is rounded to nearest: 2^-8 (bf16), 2^-24 (fp32), or in E4M3 2^-4
 of the value and 2^-10 of the scale below the smallest normal value (2^-9 where a sum's error may have doubled the scale).
@@ -196,7 +196,7 @@ def test_product(b, group, T, out):
     q, x = eight(activation(g, T, m.cols), group, "e4m3")
     z, wide, low = m.product(x)
     if out == "e4m3":
-        close8(api.bsr_linear_scaled8(m.w8, q, out_fmt="e4m3"), z, low)
+        close8(api.bsr_linear_scaled8(m.w8, q, out_fmt="e4m3"), z, wide)
         return
     y = api.bsr_linear_scaled8(m.w8, q, out_dtype=F32 if out == "f32" else BF16)
     if out == "f32":
@@ -232,8 +232,8 @@ def test_epilogue(b, T, act, residual, out):
     pre = api.empty_scaled8(T, m.rows, group=b)
     how = {"out_fmt": out} if out in ref.FORMATS else {"out_dtype": F32 if out == "f32" else BF16}
     y = api.bsr_linear_scaled8(m.w8, q, bias=bias.cuda(), act=act, residual=None if r is None else r.cuda(), pre=pre, **how)
-    z, wide, low = m.product(x)
-    off = (wide if out == "f32" else low) + 2.0 ** -22 * (z.abs() + bias.abs())
+    z, wide, _ = m.product(x)  # (Z is kept in 8 bits)
+    off = wide + 2.0 ** -22 * (z.abs() + bias.abs())
     z = z + bias.double()
     close8(pre, z, off, "kept")
     # an activation's slope is at most 1.13, its own error 2^-20 of its argument (exponential and reciprocal of a few ulps)
@@ -259,7 +259,8 @@ def test_gated(b, T, act, out, keep):
     mg, mu = (Matrix(g, masks(4, 5, s + T), b, "e4m3") for s in (1, 2))
     q, x = eight(activation(g, T, mg.cols, 0.3), 128, "e4m3")
     r = api.bsr_gated_scaled8(mg.w8, mu.w8, q, act=act, keep=keep, out_fmt=None if out == "bf16" else out)
-    (zg, _, og), (zu, _, ou) = mg.product(x), mu.product(x)
+    (zg, wg, lg), (zu, wu, lu) = mg.product(x), mu.product(x)
+    og, ou = (lg, lu) if out == "bf16" and not keep else (wg, wu)
     if keep:
         close8(r.G, zg, og, "G")
         close8(r.U, zu, ou, "U")
@@ -291,7 +292,7 @@ def test_product_of_many_tiles(b, fmts, act, residual, out, pre):
     kept = api.empty_scaled8(T, m.rows, group=b) if pre else None
     how = {"out_fmt": out} if out == "e4m3" else {"out_dtype": F32 if out == "f32" else BF16}
     y = api.bsr_linear_scaled8(m.w8, q, bias=bias.cuda(), act=act, residual=None if r is None else r.cuda(), pre=kept, **how)
-    off = (wide if out == "f32" else low) + 2.0 ** -22 * (z.abs() + bias.abs())
+    off = (low if out == "bf16" and not pre else wide) + 2.0 ** -22 * (z.abs() + bias.abs())
     z = z + bias.double()
     if pre:
         close8(kept, z, off, "kept")
@@ -312,7 +313,8 @@ def test_gated_of_many_tiles(b, act, out, keep):
     mg, mu = (Matrix(g, masks(nr, nc, s, 0.6), b, "e4m3") for s in (1, 2))
     q, x = eight(activation(g, T, mg.cols, 0.3), 128, "e4m3")
     r = api.bsr_gated_scaled8(mg.w8, mu.w8, q, act=act, keep=keep, out_fmt=None if out == "bf16" else out)
-    (zg, _, og), (zu, _, ou) = mg.product(x), mu.product(x)
+    (zg, wg, lg), (zu, wu, lu) = mg.product(x), mu.product(x)
+    og, ou = (lg, lu) if out == "bf16" and not keep else (wg, wu)
     if keep:
         close8(r.G, zg, og, "G")
         close8(r.U, zu, ou, "U")
@@ -327,6 +329,23 @@ def test_gated_of_many_tiles(b, act, out, keep):
         _, s = ref.quantised(h.numpy(), b, out)
         scale = torch.from_numpy(np.ldexp(1.0, s.astype(np.int64) - 127).T).repeat_interleave(b, 1)
         close(torch.from_numpy(ref.values(r.H.codes, r.H.scales, b, out)), h, off + 2.0 ** -3 * (h.abs() + off) + 2.0 ** -16 * scale)
+
+
+@pytest.mark.parametrize("b,T", [(64, 40), (64, 2100), (128, 40), (128, 2100)])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_eight_bit_results_are_the_fp32_ones_quantised(b, T, fmt):
+    nr, nc, _ = MANY
+    g = gen(b + T)
+    m = Matrix(g, masks(nr, nc, 5, 0.6), b, "e4m3")
+    q = api.quantize_scaled8(activation(g, T, m.cols, 0.3).cuda(), group=b)
+    bias, r = torch.randn((m.rows,), generator=g).cuda(), torch.randn((T, m.rows), generator=g).cuda()
+    kw = {"bias": bias, "act": "gelu", "residual": r}
+    z, y = api.bsr_linear_scaled8(m.w8, q, bias=bias), api.bsr_linear_scaled8(m.w8, q, **kw)
+    pre = api.empty_scaled8(T, m.rows, group=b, fmt=fmt)
+    y8 = api.bsr_linear_scaled8(m.w8, q, pre=pre, out_fmt=fmt, **kw)
+    for got, v in ((pre, z), (y8, y)):
+        want = api.quantize_scaled8(v, group=b, fmt=fmt)
+        assert torch.equal(got.codes, want.codes) and torch.equal(got.scales[:, :T], want.scales[:, :T])
 
 
 @pytest.mark.parametrize("b", [64, 128])
