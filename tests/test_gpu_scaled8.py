@@ -495,6 +495,23 @@ def test_gradient_of_the_blocks(b, group, fmt, T):
     assert torch.equal(dv, again)  # a fixed order
 
 
+@pytest.mark.parametrize("b,nbr,nbc,T", [(64, 32, 33, 17), (64, 32, 33, 512), (64, 43, 43, 530), (64, 27, 41, 513), (128, 15, 15, 1030),
+                                         (128, 12, 15, 1030), (128, 12, 15, 2500)])
+def test_gradient_of_many_blocks(b, nbr, nbc, T):
+    """A unit to a wave, the last workgroup's waves not all in use; four waves to a unit; a block to a workgroup in two runs."""
+    g = gen(nbr + T)
+    mask = torch.ones((nbr, nbc), dtype=torch.bool)
+    mask[nbr - 1, 1:] = False
+    m = Matrix(g, mask, b, "e4m3")
+    q, x = eight(activation(g, T, m.cols), b, "e5m2")
+    dy = (torch.randn((T, m.rows), generator=g) * 0.1).to(BF16)
+    dv = api.bsr_sddmm_scaled8(m.packed, dy.cuda(), q)
+    dyd, xd = dy.cuda().double(), x.cuda()
+    full, most = (dyd.t() @ xd).cpu(), (dyd.abs().t() @ xd.abs()).cpu()
+    cut = lambda f: torch.stack([f[r * b:(r + 1) * b, c * b:(c + 1) * b] for r, c in m.where])  # noqa: E731
+    close(dv, cut(full), T * 2.0 ** -24 * cut(most))
+
+
 def test_gradient_of_the_blocks_from_views():
     b, T = 64, 50
     g = gen(1)
