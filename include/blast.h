@@ -12,7 +12,9 @@
  * post-training sparsification (Sec. 3.3) and the product on 8-bit E5M2
  * operands (Sec. 5.2); and what a transformer block and its training step put next
  * to those products: bias, activation and residual in a product's epilogue, the
- * gradient through an activation, the norms with the residual add.
+ * gradient through an activation, the norms with the residual add; and all of a
+ * block's products in scaled 8-bit form, forward and backward, with the activations
+ * of a training step kept in that form.
  *
  * Conventions
  *  - Weights are `out x in`, row-major, like a linear layer's weight: W is
@@ -671,7 +673,8 @@ int blast_bsr_linear_scaled8(const blast_bsr_view* W, const blast_weight8_view* 
  *   H, ldh              out, bf16 [T][rows], may be NULL
  *   H8, G8, U8          out, scaled 8-bit, group = b, each may be NULL (not H and H8 both): what the next product, the gradients of the
  *                       blocks and blast_act_backward_scaled8 read.  The activation takes G and U before they are rounded.
- * act, operands, arithmetic (with a bf16 H alone the 8-bit instruction's) and errors as in blast_bsr_linear_scaled8; BLAST_ACT_NONE is a product of the two.
+ * act, operands, arithmetic (with a bf16 H alone the 8-bit instruction's) and errors as in blast_bsr_linear_scaled8;
+ * BLAST_ACT_NONE is a product of the two.  Wgate and Wup have one shape, block width and format.
  */
 int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_weight8_view* gate8, const blast_bsr_view* Wup,
                             const blast_weight8_view* up8, const blast_scaled8_view* X, int64_t T, int32_t act, uint16_t* H,
@@ -684,7 +687,8 @@ int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_weight8_vie
  *   dY, ldy             bf16 token-major [T][rows], 16-byte aligned, ldy % 8 == 0
  *   X                   scaled 8-bit [T][cols], group >= b, codes 16-byte aligned, ld % 16 == 0
  *   dvals               out, fp32 [nnz][b][b], 16-byte aligned; T = 0 gives zeros
- *   ws, ws_bytes        blast_bsr_sddmm_scaled8_workspace() bytes, 16-byte aligned (sums over runs of tokens, where there are few blocks)
+ *   ws, ws_bytes        blast_bsr_sddmm_scaled8_workspace() bytes, 16-byte aligned (sums over runs of tokens, where there are few blocks);
+ *                       means nothing afterwards; calls that may overlap in time have one each
  * Never synchronises.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED_BLOCK, WORKSPACE, HIP.
  */
 int blast_bsr_sddmm_scaled8(const blast_bsr_view* W, const uint16_t* dY, int64_t ldy, const blast_scaled8_view* X, int64_t T,

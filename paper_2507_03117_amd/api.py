@@ -917,7 +917,7 @@ class Scaled8:
 
 @dataclass
 class Weight8:
-    """A packed matrix with its stored blocks in 8 bits, one scale each."""
+    """A packed matrix with its stored blocks in 8 bits, one scale each: of its values when bsr_quantize_scaled8 read them."""
     packed: PackedBsr
     codes: torch.Tensor  # uint8 [nnz, b, b]
     scales: torch.Tensor  # uint8 [nnz], readable to the next multiple of 16
@@ -926,7 +926,8 @@ class Weight8:
     def view(self) -> Weight8View:
         p = self.packed
         assert self.codes.is_cuda and self.codes.dtype == torch.uint8 and self.codes.is_contiguous()
-        assert self.codes.numel() >= p.nnz * p.b * p.b and self.scales.dtype == torch.uint8 and self.scales.numel() >= p.nnz
+        assert self.codes.numel() >= p.nnz * p.b * p.b
+        assert self.scales.is_cuda and self.scales.dtype == torch.uint8 and self.scales.is_contiguous() and self.scales.numel() >= p.nnz
         return Weight8View(self.codes.data_ptr(), self.scales.data_ptr(), FORMAT8[self.fmt])
 
 

@@ -6,7 +6,8 @@
 // registers over the run and meet in LDS at its end, those of the runs in a second launch - or, for few rows, a workgroup has its
 // columns' rows to the end (k_act_backward_columns).  Measured: gated, 4096 x 14336, fp32 gradient 163 us (5.05 TB/s, the rate of a
 // large copy); GELU with the bias' gradient, 333 x 6400 7.4 us, 4096 x 6400 39 us.
-// EIGHT: Z and U in scaled 8-bit form (blast_act_backward_scaled8), a byte a value and a scale for a lane's eight.
+// EIGHT: Z and U in scaled 8-bit form (blast_act_backward_scaled8), a byte a value and a scale for a lane's eight: gated, 4096 x 14336, bf16
+// gradient 126 us (4.7 TB/s); GELU with the bias' gradient, 333 x 6400 7.7 us.
 #pragma once
 #include "kern_rows.h"
 #include "kern_scaled8.h"

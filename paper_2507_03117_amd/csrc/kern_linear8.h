@@ -9,10 +9,14 @@
 //
 // Bound, 53248 x 16384 at 95 %, 2048 tokens, bf16: bytes from beyond the L2s - a row's few blocks need other activations than the
 // next row's, so that a byte of X is fetched for every block that reads it (0.7 GB), 0.96 GB with W and the result at 6.8 TB/s; the matrix cores
-// are busy a quarter of the time.  Gated 14336 x 4096 at 95 %, 4096 tokens, G, U and H kept in 8 bits: the 176 MB of results (20 us for G and
-// U, 7 for SiLU) on top of 42 us of steps, which a row of 1.6 blocks a matrix keeps short.
+// are busy a quarter of the time.  Gated 14336 x 4096 at 95 %, 4096 tokens, G, U and H kept in 8 bits, 91 to 100 us: the 176 MB of results (20 us
+// for G and U, 7 for SiLU) on top of the steps (42 us through the 8-bit instruction, 17 more widened), which a row of 1.6 blocks a matrix
+// keeps short.  2048 x 8192 at 90 %, 64-wide, 2048 tokens, fp32 with an fp32 residual: 21 us, half of them bytes at a large copy's rate, the rest
+// widened steps.
 // k_linear8_split: eight waves have a block row's B rows of 32 tokens and deal the stored blocks among themselves, operands straight
 // into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
+// Bound: a wave's chain of row, columns, blocks and X behind a launch (14336 x 4096 at 95 %, one token 5.9 us; gated 8192 x 2048 at 90 %, 64-wide, five
+// 6.0; 1600 x 6400 at 80 %, 333 tokens, blocks dealt eight ways 11).
 #pragma once
 #include "kern_scaled8.h"
 #include "kern_stream.h"

@@ -5,6 +5,10 @@
 // (448, 57344): division by it is exact, a code depends on its value and its group's exponent alone, every value a code stands for is
 // a bf16 value (so that the gradient of the stored blocks loses nothing when it widens them), and the matrix instructions of the
 // f8f6f4 family take the exponents as they are stored.  Below 2^-100 a scale would bring code values under the smallest normal bf16.
+//
+// Bound: memory, every value read and every code written once; a lane has sixteen bytes or more of a row, a group's lanes find its maximum
+// by lane exchanges, a wave has four tokens so that their scales leave as one word (4096 x 14336, bf16: 33 us, 5.3 TB/s, a large copy's rate;
+// one token of 2048: 2.6, a launch).
 #pragma once
 #include "kern_rows.h"
 

@@ -478,6 +478,15 @@ def test_specials_stay_in_their_token(b, T):
                 assert torch.isfinite(y[1].view(3, b)[rest]).all()
 
 
+def test_scales_of_a_weight_are_contiguous_bytes():
+    m = Matrix(gen(3), masks(3, 3, 2), 64, "e4m3")
+    q = api.quantize_scaled8(torch.zeros((2, m.cols), device="cuda"), group=64)
+    n = m.packed.nnz
+    for bad in (torch.zeros((n, 2), dtype=torch.uint8, device="cuda")[:, 0], torch.zeros(n, dtype=torch.uint8), m.w8.scales[:n - 1]):
+        with pytest.raises(AssertionError):
+            api.bsr_linear_scaled8(api.Weight8(m.packed, m.w8.codes, bad), q)
+
+
 # ---- the way back -------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("b,group,fmt", [(64, 64, "e4m3"), (64, 128, "e5m2"), (128, 128, "e4m3"), (128, 128, "e5m2")])
