@@ -13,6 +13,11 @@ namespace {
 // 10.2, 256: 12.3 / 27.5; gated, 8192 x 2048 at 90 %, 128: 9.4 / 6.8, 256: 10.9 / 21.5; 14336 x 4096 at 95 %, 112: 13.6 / 14.7.
 constexpr int64_t kFewTiles = 144;
 
+// Workgroups that have 32 rows of a block row each, where no scale needs all of them: up to 32 tokens, and where whole rows would be this many
+// workgroups or fewer (us, 32 rows / whole; one token, bf16: 14336 x 4096 at 95 % 4.1 / 4.8, at 70 % 5.1 / 6.7, 4096 x 14336 at 95 % 4.0 / 5.6,
+// 64-wide 8192 x 2048 at 90 % 3.7 / 4.0; 100 tokens: 128 whole ones 6.2 / 6.4 and 64-wide 4.9 / 5.4, 448: 9.1 / 7.2, 64-wide 512: 5.3 / 4.5).
+constexpr int64_t kFewGroups = 128;
+
 int check_weight(const blast_bsr_view* W, const blast_weight8_view* W8) {
   if (!W || !W->row_ptr || !W8 || !format8_ok(W8->format)) return BLAST_ERR_INVALID_ARG;
   if (W->rows < 0 || W->cols < 0 || W->nnz < 0 || W->nnz > INT32_MAX) return BLAST_ERR_INVALID_ARG;
@@ -63,18 +68,27 @@ int raise_lds(K kernel, int bytes, blast::DeviceFlags& set) {
   return BLAST_OK;
 }
 
+template <int B, int ROWS, bool DUAL, bool EXACT, int WF, int XF>
+int launch_split(Linear8Args a, hipStream_t stream) {
+  using C = S8Cfg<B, ROWS, DUAL>;
+  static blast::DeviceFlags set;
+  if (int rc = raise_lds(&k_linear8_split<B, ROWS, DUAL, EXACT, WF, XF>, C::LDS_BYTES, set)) return rc;
+  const int64_t grid = grid8(a, C::TT, INT32_MAX);
+  if (grid == 0) return BLAST_ERR_INVALID_ARG;
+  k_linear8_split<B, ROWS, DUAL, EXACT, WF, XF><<<dim3((unsigned)grid, B / ROWS), dim3(64 * C::NW), C::LDS_BYTES, stream>>>(a);
+  BLAST_LAUNCH_CHECK("k_linear8_split");
+  return BLAST_OK;
+}
+
 template <int B, bool DUAL, bool EXACT, int WF, int XF>
 int launch_linear8(Linear8Args a, hipStream_t stream) {
   const int64_t tiles = (int64_t)a.nbr * (((int64_t)a.T + 127) / 128);
-  static blast::DeviceFlags split_set, tile_set;
+  static blast::DeviceFlags tile_set;
   if (a.T <= 32 || tiles < kFewTiles) {
-    using C = S8Cfg<B, DUAL>;
-    if (int rc = raise_lds(&k_linear8_split<B, DUAL, EXACT, WF, XF>, C::LDS_BYTES, split_set)) return rc;
-    const int64_t grid = grid8(a, C::TT, INT32_MAX);
-    if (grid == 0) return BLAST_ERR_INVALID_ARG;
-    k_linear8_split<B, DUAL, EXACT, WF, XF><<<dim3((unsigned)grid), dim3(64 * C::NW), C::LDS_BYTES, stream>>>(a);
-    BLAST_LAUNCH_CHECK("k_linear8_split");
-    return BLAST_OK;
+    if (a.y8.codes || a.k8[0].codes || a.k8[1].codes) return launch_split<B, B, DUAL, EXACT, WF, XF>(a, stream);
+    const int64_t groups = (int64_t)a.nbr * (((int64_t)a.T + 31) / 32);
+    if (a.T <= 32 || groups <= kFewGroups) return launch_split<B, 32, DUAL, EXACT, WF, XF>(a, stream);
+    return launch_split<B, B, DUAL, EXACT, WF, XF>(a, stream);
   }
   using C = L8Cfg<B>;
   if (int rc = raise_lds(&k_linear8<B, DUAL, EXACT, WF, XF>, C::LDS_BYTES, tile_set)) return rc;

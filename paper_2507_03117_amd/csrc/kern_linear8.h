@@ -13,10 +13,11 @@
 // for G and U, 7 for SiLU) on top of the steps (42 us through the 8-bit instruction, 17 more widened), which a row of 1.6 blocks a matrix
 // keeps short.  2048 x 8192 at 90 %, 64-wide, 2048 tokens, fp32 with an fp32 residual: 21 us, half of them bytes at a large copy's rate, the rest
 // widened steps.
-// k_linear8_split: eight waves have a block row's B rows of 32 tokens and deal the stored blocks among themselves, operands straight
-// into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
-// Bound: a wave's chain of row, columns, blocks and X behind a launch (14336 x 4096 at 95 %, one token 5.9 us; gated 8192 x 2048 at 90 %, 64-wide, five
-// 6.0; 1600 x 6400 at 80 %, 333 tokens, blocks dealt eight ways 11).
+// k_linear8_split: eight waves have a block row's B rows, or 32 of them, of 32 tokens and deal the stored blocks among themselves, W by way
+// of LDS in whole lines, X straight into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
+// Bound: a wave's chain of row, columns, blocks and X behind a launch (one token, 14336 x 4096 at 95 %, bf16 4.1 us, 6.0 with whole rows and W
+// straight into registers; at 70 % 5.1, 10.1 so; gated with 8-bit results 7.9 and 13.2, 8.9 and 20.4 so; 64-wide 8192 x 2048 at 90 %, gated, five
+// tokens 6.1, 6.0 so; 1600 x 6400 at 80 %, 333 tokens 7.7, 8.1 so).
 #pragma once
 #include "kern_scaled8.h"
 #include "kern_stream.h"
@@ -66,19 +67,22 @@ __device__ __forceinline__ void store_eight(const Eight& o, const float (&v)[8],
   }
 }
 
-// Eight rows of a token from the sums to the outputs.
-template <int B, bool DUAL>
+// Eight rows of a token from the sums to the outputs.  WHOLE: the workgroup has all B rows of it, which a scale is made of.
+template <int B, bool DUAL, bool WHOLE>
 __device__ __forceinline__ void linear8_finish(const Linear8Args& a, float (&z)[8], float (&u)[8], const float (&bias)[8], int64_t t,
                                                int64_t row, bool live) {
   if constexpr (DUAL) {
-    if (a.k8[0].codes) store_eight<B>(a.k8[0], z, t, row, live);
-    if (a.k8[1].codes) store_eight<B>(a.k8[1], u, t, row, live);
+    if constexpr (WHOLE)
+      if (a.k8[0].codes) store_eight<B>(a.k8[0], z, t, row, live);
+    if constexpr (WHOLE)
+      if (a.k8[1].codes) store_eight<B>(a.k8[1], u, t, row, live);
 #pragma unroll
     for (int j = 0; j < 8; ++j) z[j] = (a.act >= 0 ? epilogue_act(a.act, z[j]) : z[j]) * u[j];
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) z[j] += bias[j];
-    if (a.k8[0].codes) store_eight<B>(a.k8[0], z, t, row, live);
+    if constexpr (WHOLE)
+      if (a.k8[0].codes) store_eight<B>(a.k8[0], z, t, row, live);
     if (a.act >= 0) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] = epilogue_act(a.act, z[j]);
@@ -98,7 +102,8 @@ __device__ __forceinline__ void linear8_finish(const Linear8Args& a, float (&z)[
       for (int j = 0; j < 8; ++j) z[j] += r[j];
     }
   }
-  if (a.y8.codes) store_eight<B>(a.y8, z, t, row, live);
+  if constexpr (WHOLE)
+    if (a.y8.codes) store_eight<B>(a.y8, z, t, row, live);
   if (a.y && live) {
     unsigned char* p = row_of(a.y, t * a.ldy + row, a.y_bf16);
     if (a.y_vec)
@@ -728,16 +733,20 @@ __global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
 
 // ---- few tiles: waves share the stored blocks of a block row ------------------------------------------------------------------
 
-template <int B, bool DUAL>
+template <int B, int ROWS, bool DUAL>
 struct S8Cfg {
-  static constexpr int NW = 8, TT = 32, RT = B / 32;
-  static constexpr int EP_TOKENS = DUAL && B == 128 ? 16 : 32;  // tokens whose sums lie in LDS at once, of every wave and matrix
-  static constexpr int LDS_BYTES = NW * EP_TOKENS * B * 4 * (DUAL ? 2 : 1);
+  static constexpr int NW = 8, TT = 32, RT = ROWS / 32;
+  static constexpr int EP_TOKENS = DUAL && ROWS == 128 ? 16 : 32;  // tokens whose sums lie in LDS at once, of every wave and matrix
+  static constexpr int W_BYTES = ROWS * B;  // a wave's block
+  static constexpr int SUM_BYTES = NW * EP_TOKENS * ROWS * 4 * (DUAL ? 2 : 1), LDS_BYTES = SUM_BYTES > NW * W_BYTES ? SUM_BYTES : NW * W_BYTES;
+  // 16-byte chunk c of a row lies at c ^ key(row): eight rows' chunks of a fragment are on different banks.
+  __device__ static __forceinline__ int key(int row) { return B == 128 ? row & 7 : (row >> 1) & 3; }
 };
 
-template <int B, bool DUAL, bool EXACT, int WF, int XF>
+// ROWS: of a block row's B, the workgroup's (blockIdx.y says which).  The sums are the same in either form.
+template <int B, int ROWS, bool DUAL, bool EXACT, int WF, int XF>
 __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
-  using C = S8Cfg<B, DUAL>;
+  using C = S8Cfg<B, ROWS, DUAL>;
   constexpr int NM = DUAL ? 2 : 1, RT = C::RT, NW = C::NW, KS = B / 64;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -763,47 +772,80 @@ __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[m][i][0][v] = 0.0f;
 
-  auto block = [&](f32x16 (&d)[RT][1], const Mat8& m, int q) {
+  // W by way of LDS, a block to a wave's own part of it: whole lines are asked for, where a fragment's 32 bytes a row would ask for each
+  // line again and again.  The next block is on its way beside the matrix instructions.
+  unsigned char* mine = smem + wave * C::W_BYTES;
+  struct Ahead {
+    i32x8 x[KS];
+    int xs, ws;
+  };
+  auto ask = [&](Ahead& n, const Mat8& m, int q) {
+    constexpr int kSlots = B / 16;
+    const uint8_t* w = m.vals + (int64_t)q * (B * B) + (int)blockIdx.y * ROWS * B;
+#pragma unroll
+    for (int i = 0; i < C::W_BYTES / 1024; ++i) {
+      const int row = i * (64 / kSlots) + lane / kSlots;
+      BLAST_GLDS16(w + row * B + (((lane % kSlots) ^ C::key(row)) << 4), mine + i * 1024);
+    }
     const int c = ld_idx(m.col_idx, q);
-    const int ws = (ld_idx(reinterpret_cast<const int*>(m.scales), q >> 2) >> (8 * (q & 3))) & 255;
-    const uint8_t* w = m.vals + (int64_t)q * (B * B) + l32 * B + lh * 32;
+    n.ws = (ld_idx(reinterpret_cast<const int*>(m.scales), q >> 2) >> (8 * (q & 3))) & 255;
+    n.xs = a.x.scales[(((int64_t)c * B) >> a.x.shift) * a.x.lds + t];
     const uint8_t* x = xrow + (int64_t)c * B;
-    const int xs[1] = {a.x.scales[(((int64_t)c * B) >> a.x.shift) * a.x.lds + t]};
-    i32x8 fw[KS][RT], fx[KS][1];
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-#pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const i32x4* p = reinterpret_cast<const i32x4*>(w + i * 32 * B + k * 64);
-        fw[k][i] = __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
-      }
       const i32x4* p = reinterpret_cast<const i32x4*>(x + k * 64);
-      fx[k][0] = __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      n.x[k] = __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
     }
+  };
+  auto blocks = [&](f32x16 (&d)[RT][1], const Mat8& m, int first, int q0, int n) {
+    if (first >= n) return;
+    Ahead next;
+    ask(next, m, q0 + first);
+#pragma unroll 1
+    for (int e = first; e < n; e += NW) {
+      const Ahead now = next;
+      const int xs[1] = {now.xs};
+      __builtin_amdgcn_s_waitcnt(BLAST_VMCNT(0));
+      asm volatile("" ::: "memory");
 #pragma unroll
-    for (int k = 0; k < KS; ++k) multiply8<RT, 1, EXACT, WF, XF>(d, fw[k], fx[k], ws, xs);
+      for (int k = 0; k < KS; ++k) {
+        i32x8 fw[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          const int row = i * 32 + l32;
+          i32x4 h[2];
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            h[p] = *reinterpret_cast<const i32x4*>(mine + row * B + (((k * 4 + lh * 2 + p) ^ C::key(row)) << 4));
+          fw[i] = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        if (k == KS - 1 && e + NW < n) {
+          __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the part is read before it is written again
+          asm volatile("" ::: "memory");
+          ask(next, m, q0 + e + NW);
+        }
+        const i32x8 fx[1] = {now.x[k]};
+        multiply8<RT, 1, EXACT, WF, XF>(d, fw, fx, now.ws, xs);
+      }
+    }
   };
   // the blocks of both matrices are dealt as one sequence
-#pragma unroll 1
-  for (int e = wave; e < nb[0]; e += NW) block(acc[0], a.m[0], kb[0] + e);
-  if constexpr (DUAL) {
-#pragma unroll 1
-    for (int e = (wave + NW - nb[0] % NW) % NW; e < nb[1]; e += NW) block(acc[1], a.m[1], kb[1] + e);
-  }
+  blocks(acc[0], a.m[0], wave, kb[0], nb[0]);
+  if constexpr (DUAL) blocks(acc[1], a.m[1], (wave + NW - nb[0] % NW) % NW, kb[1], nb[1]);
 
   const int all = nb[0] + (DUAL ? nb[NM - 1] : 0), waves = all < NW ? (all < 1 ? 1 : all) : NW;  // those that have sums
-  constexpr int kPieces = B / 8, kRows = 64 * NW / kPieces, PITCH = B * 4, SET = C::EP_TOKENS * PITCH;
+  constexpr int kPieces = ROWS / 8, kRows = 64 * NW / kPieces, PITCH = ROWS * 4, SET = C::EP_TOKENS * PITCH;
   const int piece = threadIdx.x % kPieces;
-  const int64_t row = (int64_t)r * B + piece * 8;
+  const int64_t row = (int64_t)r * B + (int)blockIdx.y * ROWS + piece * 8;
   float bias[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) bias[j] = !DUAL && a.bias ? a.bias[row + j] : 0.0f;
-#pragma unroll
+#pragma unroll 1
   for (int pass = 0; pass < C::TT / C::EP_TOKENS; ++pass) {
     if (t0 + pass * C::EP_TOKENS >= a.T) break;
-    if (pass > 0) __syncthreads();
+    __syncthreads();
     const int tok = l32 - pass * C::EP_TOKENS;
-    if (wave < waves && tok >= 0 && tok < C::EP_TOKENS) {
+    if (wave < waves && tok >= 0 && tok < C::EP_TOKENS && t0 + l32 < a.T) {
 #pragma unroll
       for (int m = 0; m < NM; ++m) {
         unsigned char* base = smem + (wave * NM + m) * SET + tok * PITCH;
@@ -827,16 +869,24 @@ __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = 0.0f;
 #pragma unroll 1
-        for (int w = 0; w < waves; ++w) {
-          const unsigned char* base = smem + (w * NM + m) * SET + k * PITCH;
-          const float4 lo = *reinterpret_cast<const float4*>(base + (((2 * piece) ^ (k & 7)) << 4));
-          const float4 hi = *reinterpret_cast<const float4*>(base + (((2 * piece + 1) ^ (k & 7)) << 4));
-          v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w, v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
+        for (int w0 = 0; w0 < waves; w0 += 2) {  // two at a time: their reads are under way together
+          float4 lo[2], hi[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const unsigned char* base = smem + ((w0 + i) * NM + m) * SET + k * PITCH;
+            lo[i] = *reinterpret_cast<const float4*>(base + (((2 * piece) ^ (k & 7)) << 4));
+            hi[i] = *reinterpret_cast<const float4*>(base + (((2 * piece + 1) ^ (k & 7)) << 4));
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (i == 0 || w0 + i < waves)
+              v[0] += lo[i].x, v[1] += lo[i].y, v[2] += lo[i].z, v[3] += lo[i].w, v[4] += hi[i].x, v[5] += hi[i].y, v[6] += hi[i].z,
+                  v[7] += hi[i].w;
         }
       };
       take(0, z);
       if constexpr (DUAL) take(1, u);
-      linear8_finish<B, DUAL>(a, z, u, bias, tk, row, tk < a.T);
+      linear8_finish<B, DUAL, ROWS == B>(a, z, u, bias, tk, row, tk < a.T);
     }
   }
 }
