@@ -17,7 +17,7 @@
 // of LDS in whole lines, X straight into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
 // Bound: a wave's chain of row, columns, blocks and X behind a launch (one token, 14336 x 4096 at 95 %, bf16 4.1 us, 6.0 with whole rows and W
 // straight into registers; at 70 % 5.1, 10.1 so; gated with 8-bit results 7.9 and 13.2, 8.9 and 20.4 so; 64-wide 8192 x 2048 at 90 %, gated, five
-// tokens 6.1, 6.0 so; 1600 x 6400 at 80 %, 333 tokens 7.7, 8.1 so).
+// tokens 6.1, 6.0 so; 1600 x 6400 at 80 %, 333 tokens 7.7, 8.1 so; with bias and bf16 residual 9.4, 11 where they were asked for behind the sums).
 #pragma once
 #include "kern_scaled8.h"
 #include "kern_stream.h"
@@ -67,10 +67,19 @@ __device__ __forceinline__ void store_eight(const Eight& o, const float (&v)[8],
   }
 }
 
+// Eight rows of a token of the residual, asked for.
+__device__ __forceinline__ void ask_residual(const Linear8Args& a, Piece& q, int64_t t, int64_t row) {
+  const unsigned char* p = row_of(a.r, t * a.ldr + row, a.r_bf16);
+  if (a.r_vec)
+    piece_load<1, true>(q, p, 0, 0, 8, a.r_bf16);
+  else
+    piece_load<1, false>(q, p, 0, 0, 8, a.r_bf16);
+}
+
 // Eight rows of a token from the sums to the outputs.  WHOLE: the workgroup has all B rows of it, which a scale is made of.
 template <int B, bool DUAL, bool WHOLE>
-__device__ __forceinline__ void linear8_finish(const Linear8Args& a, float (&z)[8], float (&u)[8], const float (&bias)[8], int64_t t,
-                                               int64_t row, bool live) {
+__device__ __forceinline__ void linear8_finish(const Linear8Args& a, float (&z)[8], float (&u)[8], const float (&bias)[8],
+                                               const Piece& residual, int64_t t, int64_t row, bool live) {
   if constexpr (DUAL) {
     if constexpr (WHOLE)
       if (a.k8[0].codes) store_eight<B>(a.k8[0], z, t, row, live);
@@ -88,16 +97,11 @@ __device__ __forceinline__ void linear8_finish(const Linear8Args& a, float (&z)[
       for (int j = 0; j < 8; ++j) z[j] = epilogue_act(a.act, z[j]);
     }
     if (a.r && live) {
-      Piece q{};
       float r[8];
-      const unsigned char* p = row_of(a.r, t * a.ldr + row, a.r_bf16);
-      if (a.r_vec) {
-        piece_load<1, true>(q, p, 0, 0, 8, a.r_bf16);
-        piece_values<true>(q, a.r_bf16, r);
-      } else {
-        piece_load<1, false>(q, p, 0, 0, 8, a.r_bf16);
-        piece_values<false>(q, a.r_bf16, r);
-      }
+      if (a.r_vec)
+        piece_values<true>(residual, a.r_bf16, r);
+      else
+        piece_values<false>(residual, a.r_bf16, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] += r[j];
     }
@@ -764,6 +768,21 @@ __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
   const int64_t t = t0 + l32 < a.T ? t0 + l32 : a.T - 1;  // (lanes beyond the last token repeat it; nothing of them is stored)
   const uint8_t* xrow = a.x.codes + t * a.x.ld + lh * 32;
 
+  constexpr int kPieces = ROWS / 8, kRows = 64 * NW / kPieces, PITCH = ROWS * 4, SET = C::EP_TOKENS * PITCH;
+  const int piece = threadIdx.x % kPieces;
+  const int64_t row = (int64_t)r * B + (int)blockIdx.y * ROWS + piece * 8;
+  // what a thread adds to its sums (of one token, if there is anything to add), on its way from the start
+  float bias[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  Piece residual{};
+  if constexpr (!DUAL) {
+    static_assert(kRows >= C::EP_TOKENS && C::EP_TOKENS == C::TT, "");
+    if (a.bias) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) bias[j] = a.bias[row + j];
+    }
+    const int64_t tk = t0 + (int)threadIdx.x / kPieces;
+    if (a.r && (int)threadIdx.x / kPieces < C::TT && tk < a.T) ask_residual(a, residual, tk, row);
+  }
   f32x16 acc[NM][RT][1];
 #pragma unroll
   for (int m = 0; m < NM; ++m)
@@ -834,12 +853,6 @@ __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
   if constexpr (DUAL) blocks(acc[1], a.m[1], (wave + NW - nb[0] % NW) % NW, kb[1], nb[1]);
 
   const int all = nb[0] + (DUAL ? nb[NM - 1] : 0), waves = all < NW ? (all < 1 ? 1 : all) : NW;  // those that have sums
-  constexpr int kPieces = ROWS / 8, kRows = 64 * NW / kPieces, PITCH = ROWS * 4, SET = C::EP_TOKENS * PITCH;
-  const int piece = threadIdx.x % kPieces;
-  const int64_t row = (int64_t)r * B + (int)blockIdx.y * ROWS + piece * 8;
-  float bias[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) bias[j] = !DUAL && a.bias ? a.bias[row + j] : 0.0f;
 #pragma unroll 1
   for (int pass = 0; pass < C::TT / C::EP_TOKENS; ++pass) {
     if (t0 + pass * C::EP_TOKENS >= a.T) break;
@@ -886,7 +899,7 @@ __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
       };
       take(0, z);
       if constexpr (DUAL) take(1, u);
-      linear8_finish<B, DUAL, ROWS == B>(a, z, u, bias, tk, row, tk < a.T);
+      linear8_finish<B, DUAL, ROWS == B>(a, z, u, bias, residual, tk, row, tk < a.T);
     }
   }
 }
