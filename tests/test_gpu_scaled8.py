@@ -348,6 +348,22 @@ def test_eight_bit_results_are_the_fp32_ones_quantised(b, T, fmt):
         assert torch.equal(got.codes, want.codes) and torch.equal(got.scales[:, :T], want.scales[:, :T])
 
 
+@pytest.mark.parametrize("b,nr,nc,T", [(64, 3, 40, 1), (64, 3, 9, 20), (128, 3, 20, 1), (128, 2, 9, 32), (128, 130, 3, 33), (64, 130, 3, 33)])
+def test_results_of_few_tokens_are_the_same_in_every_form(b, nr, nc, T):
+    """fp32 results come from parts of a block row, 8-bit ones from whole rows: rows of more blocks than waves, and of none."""
+    g = gen(b + nr + T)
+    m = Matrix(g, masks(nr, nc, 5, 0.8), b, "e4m3")
+    q = api.quantize_scaled8(activation(g, T, m.cols, 0.3).cuda(), group=b)
+    bias = torch.randn((m.rows,), generator=g).cuda()
+    r = torch.randn((T, m.rows), generator=g).cuda()
+    y = api.bsr_linear_scaled8(m.w8, q, bias=bias, act="silu", residual=r)
+    y8 = api.bsr_linear_scaled8(m.w8, q, bias=bias, act="silu", residual=r, out_fmt="e4m3")
+    want = api.quantize_scaled8(y, group=b)
+    assert torch.equal(y8.codes, want.codes) and torch.equal(y8.scales[:, :T], want.scales[:, :T])
+    into = r.clone()  # the residual in place
+    assert torch.equal(api.bsr_linear_scaled8(m.w8, q, bias=bias, act="silu", residual=into, out=into), y)
+
+
 @pytest.mark.parametrize("b", [64, 128])
 @pytest.mark.parametrize("tiles", [1, 17])
 def test_results_are_rounded_like_the_quantiser(b, tiles):
