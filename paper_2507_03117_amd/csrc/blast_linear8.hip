@@ -8,10 +8,11 @@ using namespace blast_dev;
 namespace {
 
 // Fewer 128-token tiles than this are cut into tiles of 32 whose blocks eight waves share, and up to 32 tokens any number.  Microseconds
-// of 128-token tiles / of 32, with the number of the former: 2048 x 8192 at 90 %, 64-wide, fp32, 16 tiles 12.2 / 6.6, 64: 14.5 / 9.3, 128:
-// 15.0 / 11.5, 256: 16.6 / 20.2; 1600 x 6400 at 80 %, 75: 17.7 / 11.0, 200: 18.5 / 20.0; 4096 x 14336 at 95 %, 128-wide, bf16, 64: 11.0 /
-// 10.2, 256: 12.3 / 27.5; gated, 8192 x 2048 at 90 %, 128: 9.4 / 6.8, 256: 10.9 / 21.5; 14336 x 4096 at 95 %, 112: 13.6 / 14.7.
-constexpr int64_t kFewTiles = 144;
+// of 128-token tiles / of 32, 8-bit results, with the number of the former.  64-wide, 2048 x 8192 at 90 %, 32 tiles 11.8 / 5.3, 128: 11.9 / 7.0;
+// 6400 x 1600 at 80 %, 200: 8.7 / 7.4, 300: 8.9 / 9.6; 8192 x 2048 at 50 %, 256: 14.2 / 12.3; gated, 2048 x 8192, 128: 20 / 15, 6400 x 1600, 200: 12.7 /
+// 18.6.  128-wide, 4096 x 14336 at 95 %, 128: 13.7 / 10.8, 14336 x 4096, 112: 9.9 / 7.6, 224: 9.9 / 12.7; gated 112: 13.6 / 16.4, at 70 % 35 / 31.
+template <int B, bool DUAL>
+constexpr int64_t kFewTiles = B == 64 && !DUAL ? 257 : 144;
 
 // Workgroups that have 32 rows of a block row each, where no scale needs all of them: up to 32 tokens, and where whole rows would be this many
 // workgroups or fewer (us, 32 rows / whole; one token, bf16: 14336 x 4096 at 95 % 4.1 / 4.8, at 70 % 5.1 / 6.7, 4096 x 14336 at 95 % 4.0 / 5.6,
@@ -84,7 +85,7 @@ template <int B, bool DUAL, bool EXACT, int WF, int XF>
 int launch_linear8(Linear8Args a, hipStream_t stream) {
   const int64_t tiles = (int64_t)a.nbr * (((int64_t)a.T + 127) / 128);
   static blast::DeviceFlags tile_set;
-  if (a.T <= 32 || tiles < kFewTiles) {
+  if (a.T <= 32 || tiles < kFewTiles<B, DUAL>) {
     if (a.y8.codes || a.k8[0].codes || a.k8[1].codes) return launch_split<B, B, DUAL, EXACT, WF, XF>(a, stream);
     const int64_t groups = (int64_t)a.nbr * (((int64_t)a.T + 31) / 32);
     if (a.T <= 32 || groups <= kFewGroups) return launch_split<B, 32, DUAL, EXACT, WF, XF>(a, stream);

@@ -17,7 +17,7 @@ def plain_weight(g, nr, nc, b, keep=0.6):
 
 
 @pytest.mark.parametrize("b", [64, 128])
-@pytest.mark.parametrize("T", [5, 2560])
+@pytest.mark.parametrize("T", [5, 2560, 4200])
 def test_rows_of_more_than_64_blocks(b, T):
     """Full rows of 70 blocks, an odd 67 and none, by waves that share them and by tiles."""
     g = gen(b)
