@@ -657,10 +657,9 @@ int blast_bsr_quantize_scaled8(const blast_bsr_view* W, int32_t format, uint8_t*
  *   Y, ldy, y_dtype     out, fp32 or bf16, may be NULL; may be R (same pitch and type)
  *   Y8                  out, the same values in scaled 8-bit form, group = b, codes and pitch as X; may be NULL
  *   Z8                  out, Z in scaled 8-bit form, likewise; may be NULL: what blast_act_backward_scaled8 reads
- * Products are summed in fp32; bias, activation and residual are added in fp32, with one rounding when a value is stored.  A call with an
- * fp32 or 8-bit result multiplies the exactly widened codes, at the 16-bit matrix instruction's rate: its 8-bit results are what
- * blast_quantize_scaled8 makes of its fp32 ones.  With bf16 results alone the products come from the 8-bit instruction, which drops low
- * bits of a product next to larger ones: root mean square error 1.5e-5 of a sum, 1/130 of bf16's half step.
+ * The codes are widened exactly and multiplied by the 16-bit matrix instruction; sums are held in fp32, bias, activation and residual are
+ * added in fp32, with one rounding when a value is stored: bf16 results are the fp32 ones rounded, 8-bit ones what blast_quantize_scaled8 makes of the
+ * fp32 ones, and neither depends on what else the call writes.
  * Rows are never cut into chunks: sums have a fixed order.  No output overlaps another or an input, R = Y apart.
  * Never synchronises.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED_BLOCK, HIP.
  */
@@ -673,7 +672,7 @@ int blast_bsr_linear_scaled8(const blast_bsr_view* W, const blast_weight8_view* 
  *   H, ldh              out, bf16 [T][rows], may be NULL
  *   H8, G8, U8          out, scaled 8-bit, group = b, each may be NULL (not H and H8 both): what the next product, the gradients of the
  *                       blocks and blast_act_backward_scaled8 read.  The activation takes G and U before they are rounded.
- * act, operands, arithmetic (with a bf16 H alone the 8-bit instruction's) and errors as in blast_bsr_linear_scaled8;
+ * act, operands, arithmetic and errors as in blast_bsr_linear_scaled8;
  * BLAST_ACT_NONE is a product of the two.  Wgate and Wup have one shape, block width and format.
  */
 int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_weight8_view* gate8, const blast_bsr_view* Wup,

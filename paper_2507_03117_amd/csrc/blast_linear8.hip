@@ -8,15 +8,18 @@ using namespace blast_dev;
 namespace {
 
 // Fewer 128-token tiles than this are cut into tiles of 32 whose blocks eight waves share, and up to 32 tokens any number.  Microseconds
-// of 128-token tiles / of 32, 8-bit results, with the number of the former.  64-wide, 2048 x 8192 at 90 %, 32 tiles 11.8 / 5.3, 128: 11.9 / 7.0;
-// 6400 x 1600 at 80 %, 200: 8.7 / 7.4, 300: 8.9 / 9.6; 8192 x 2048 at 50 %, 256: 14.2 / 12.3; gated, 2048 x 8192, 128: 20 / 15, 6400 x 1600, 200: 12.7 /
-// 18.6.  128-wide, 4096 x 14336 at 95 %, 128: 13.7 / 10.8, 14336 x 4096, 112: 9.9 / 7.6, 224: 9.9 / 12.7; gated 112: 13.6 / 16.4, at 70 % 35 / 31.
+// of 128-token tiles / of 32, bf16 results (8-bit ones within 4 %, fp32 ones 1 to 5 us more on both sides), with the number of the former.  64-wide,
+// 2048 x 8192 at 90 %, 64 tiles 13.8 / 6.7, 192: 14.7 / 12.8, 256: 15.1 / 14.6, 288: 16.0 / 16.9; 6400 x 1600 at 80 %, 200: 9.0 / 7.8, 300: 9.3 / 10.6; 1600 x
+// 6400 at 80 %, 225: 18.7 / 18.0, 250: 18.9 / 19.4; 8192 x 2048 at 50 %, 256, a tile to a CU: 16.2 / 14.7.  Gated, 2048 x 8192, 128: 22.8 / 17.2, 192: 23.6 / 23.9;
+// 6400 x 1600, 100: 13.3 / 10.7, 200: 14.0 / 19.4.  128-wide, 4096 x 14336 at 95 %, 128: 16.7 / 12.9, 192: 16.8 / 17.9, at 70 %, 128: 49 / 31, 192: 49 / 45, 224:
+// 50 / 55; 14336 x 4096 at 95 %, 112: 9.8 / 7.8, 224: 10.7 / 13.9; gated 112: 16.7 / 16.7, at 70 % 38 / 32; 4096 x 14336, 128: 27.4 / 27.6, at 70 % 91 / 62.
 template <int B, bool DUAL>
-constexpr int64_t kFewTiles = B == 64 && !DUAL ? 257 : 144;
+constexpr int64_t kFewTiles = B == 64 && !DUAL ? 256 : 144;
 
 // Workgroups that have 32 rows of a block row each, where no scale needs all of them: up to 32 tokens, and where whole rows would be this many
-// workgroups or fewer (us, 32 rows / whole; one token, bf16: 14336 x 4096 at 95 % 4.1 / 4.8, at 70 % 5.1 / 6.7, 4096 x 14336 at 95 % 4.0 / 5.6,
-// 64-wide 8192 x 2048 at 90 % 3.7 / 4.0; 100 tokens: 128 whole ones 6.2 / 6.4 and 64-wide 4.9 / 5.4, 448: 9.1 / 7.2, 64-wide 512: 5.3 / 4.5).
+// workgroups or fewer (us, 32 rows / whole; bf16; one token: 14336 x 4096 at 95 % 4.2 / 5.4, at 70 % 7.6 / 9.5, 4096 x 14336 at 95 % 4.2 / 6.5, 64-wide
+// 8192 x 2048 at 90 % 3.7 / 4.1; 100 tokens: 4096 x 14336 at 95 %, 128 whole ones 6.9 / 7.2, at 70 % 17.9 / 16.8, 64-wide 2048 x 8192 at 90 % 5.2 / 5.6; 14336 x 4096 at
+// 95 %, 448: 9.4 / 7.7, 64-wide 8192 x 2048, 512: 6.2 / 5.0).
 constexpr int64_t kFewGroups = 128;
 
 int check_weight(const blast_bsr_view* W, const blast_weight8_view* W8) {
@@ -47,8 +50,8 @@ int cu_count8() {
 }
 
 // Workgroups for tiles of TT tokens: one for each, or as many as are resident at once; 0: more tiles than can be counted.  Many tiles: two
-// XCDs share a block row, each with half of its tokens (53248 x 16384 at 95 %, 2048 tokens, one / two / four / eight XCDs to a row: 148 /
-// 142 / 149 / 154 us; gated 14336 x 4096, 4096 tokens 85 / 84 / 85 / 84).  An odd number of tiles leaves one of two XCDs a tile short.
+// XCDs share a block row, each with half of its tokens (us, one / two / four / eight XCDs to a row: 53248 x 16384 at 95 %, 2048 tokens 191 / 189 / 191 /
+// 192; gated 14336 x 4096, 4096 tokens 99 / 100 / 100 / 99; 2048 x 8192 at 90 %, 64-wide, 2048 tokens 24.0 / 22.8 / 22.2 / 22.0).  An odd number of tiles leaves one of two XCDs a tile short.
 int64_t grid8(Linear8Args& a, int TT, int64_t resident) {
   a.ntt = (int)(((int64_t)a.T + TT - 1) / TT);
   a.parts = TT >= 128 && a.ntt >= 2 && (a.ntt % 2 == 0 || a.ntt >= 16) ? 2 : 1;
@@ -69,46 +72,42 @@ int raise_lds(K kernel, int bytes, blast::DeviceFlags& set) {
   return BLAST_OK;
 }
 
-template <int B, int ROWS, bool DUAL, bool EXACT, int WF, int XF>
+template <int B, int ROWS, bool DUAL, int WF, int XF>
 int launch_split(Linear8Args a, hipStream_t stream) {
   using C = S8Cfg<B, ROWS, DUAL>;
   static blast::DeviceFlags set;
-  if (int rc = raise_lds(&k_linear8_split<B, ROWS, DUAL, EXACT, WF, XF>, C::LDS_BYTES, set)) return rc;
+  if (int rc = raise_lds(&k_linear8_split<B, ROWS, DUAL, WF, XF>, C::LDS_BYTES, set)) return rc;
   const int64_t grid = grid8(a, C::TT, INT32_MAX);
   if (grid == 0) return BLAST_ERR_INVALID_ARG;
-  k_linear8_split<B, ROWS, DUAL, EXACT, WF, XF><<<dim3((unsigned)grid, B / ROWS), dim3(64 * C::NW), C::LDS_BYTES, stream>>>(a);
+  k_linear8_split<B, ROWS, DUAL, WF, XF><<<dim3((unsigned)grid, B / ROWS), dim3(64 * C::NW), C::LDS_BYTES, stream>>>(a);
   BLAST_LAUNCH_CHECK("k_linear8_split");
   return BLAST_OK;
 }
 
-template <int B, bool DUAL, bool EXACT, int WF, int XF>
+template <int B, bool DUAL, int WF, int XF>
 int launch_linear8(Linear8Args a, hipStream_t stream) {
   const int64_t tiles = (int64_t)a.nbr * (((int64_t)a.T + 127) / 128);
   static blast::DeviceFlags tile_set;
   if (a.T <= 32 || tiles < kFewTiles<B, DUAL>) {
-    if (a.y8.codes || a.k8[0].codes || a.k8[1].codes) return launch_split<B, B, DUAL, EXACT, WF, XF>(a, stream);
+    if (a.y8.codes || a.k8[0].codes || a.k8[1].codes) return launch_split<B, B, DUAL, WF, XF>(a, stream);
     const int64_t groups = (int64_t)a.nbr * (((int64_t)a.T + 31) / 32);
-    if (a.T <= 32 || groups <= kFewGroups) return launch_split<B, 32, DUAL, EXACT, WF, XF>(a, stream);
-    return launch_split<B, B, DUAL, EXACT, WF, XF>(a, stream);
+    if (a.T <= 32 || groups <= kFewGroups) return launch_split<B, 32, DUAL, WF, XF>(a, stream);
+    return launch_split<B, B, DUAL, WF, XF>(a, stream);
   }
   using C = L8Cfg<B>;
-  if (int rc = raise_lds(&k_linear8<B, DUAL, EXACT, WF, XF>, C::LDS_BYTES, tile_set)) return rc;
+  if (int rc = raise_lds(&k_linear8<B, DUAL, WF, XF>, C::LDS_BYTES, tile_set)) return rc;
   const int64_t grid = grid8(a, C::TT, 2 * cu_count8());
   if (grid == 0) return BLAST_ERR_INVALID_ARG;
-  k_linear8<B, DUAL, EXACT, WF, XF><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a);
+  k_linear8<B, DUAL, WF, XF><<<dim3((unsigned)grid), dim3(256), C::LDS_BYTES, stream>>>(a);
   BLAST_LAUNCH_CHECK("k_linear8");
   return BLAST_OK;
 }
 
-// EXACT: products of the codes widened to bf16.  For fp32 results and for those in 8 bits, whose codes are then those of a sum in 32
-// bits (through the 8-bit instruction one code in a thousand is the neighbouring one, and now and then a scale its double: 53248 x 16384
-// at 95 %, 2048 tokens, 8-bit result 143 us so, 203 exactly; gated 14336 x 4096, 4096 tokens, G, U and H kept 84 / 101, one or five tokens the
-// same).  A bf16 result's own rounding is 130 times the 8-bit instruction's.
-template <int B, bool DUAL, bool EXACT>
+template <int B, bool DUAL>
 int by_formats(const Linear8Args& a, hipStream_t stream) {
   if (a.wfmt == BLAST_E4M3)
-    return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, EXACT, 0, 0>(a, stream) : launch_linear8<B, DUAL, EXACT, 0, 1>(a, stream);
-  return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, EXACT, 1, 0>(a, stream) : launch_linear8<B, DUAL, EXACT, 1, 1>(a, stream);
+    return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, 0, 0>(a, stream) : launch_linear8<B, DUAL, 0, 1>(a, stream);
+  return a.x.fmt == BLAST_E4M3 ? launch_linear8<B, DUAL, 1, 0>(a, stream) : launch_linear8<B, DUAL, 1, 1>(a, stream);
 }
 
 }  // namespace
@@ -150,8 +149,7 @@ extern "C" int blast_bsr_linear_scaled8(const blast_bsr_view* W, const blast_wei
   a.y_vec = blast::aligned(Y, 16) && ldy * (a.y_bf16 ? 2 : 4) % 16 == 0;
   if (Y8) a.y8 = eight_of(Y8);
   if (Z8) a.k8[0] = eight_of(Z8);
-  if ((Y && !a.y_bf16) || Y8 || Z8) return W->b == 64 ? by_formats<64, false, true>(a, stream) : by_formats<128, false, true>(a, stream);
-  return W->b == 64 ? by_formats<64, false, false>(a, stream) : by_formats<128, false, false>(a, stream);
+  return W->b == 64 ? by_formats<64, false>(a, stream) : by_formats<128, false>(a, stream);
 }
 
 extern "C" int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_weight8_view* gate8, const blast_bsr_view* Wup,
@@ -190,6 +188,5 @@ extern "C" int blast_bsr_gated_scaled8(const blast_bsr_view* Wgate, const blast_
   if (H8) a.y8 = eight_of(H8);
   if (G8) a.k8[0] = eight_of(G8);
   if (U8) a.k8[1] = eight_of(U8);
-  if (H8 || G8 || U8) return Wgate->b == 64 ? by_formats<64, true, true>(a, stream) : by_formats<128, true, true>(a, stream);
-  return Wgate->b == 64 ? by_formats<64, true, false>(a, stream) : by_formats<128, true, false>(a, stream);
+  return Wgate->b == 64 ? by_formats<64, true>(a, stream) : by_formats<128, true>(a, stream);
 }

@@ -5,19 +5,20 @@
 // k_linear8: workgroups of four waves, two on a CU, walk lists of tiles: a block row's B rows of 128 tokens.  A step is 128 of the
 // contraction: a stored block of 128 x 128 or two of 64 x 64, W and X tiles copied to LDS in rows of 128 bytes, the scales of the step's
 // tokens beside them; the next step's copies are under way while one is multiplied, the next tile's first step while a tile's results
-// leave (53248 x 16384 at 95 %, 2048 tokens, a workgroup for each tile 148 us, lists 142; gated 14336 x 4096, 4096 tokens, 84 / 82).
+// leave (passes on the GPU alone: 53248 x 16384 at 95 %, 2048 tokens, a workgroup for each tile 199 us, lists 189; gated 14336 x 4096, 4096 tokens, 106 /
+// 100).
 //
-// Bound, 53248 x 16384 at 95 %, 2048 tokens, bf16: bytes from beyond the L2s - a row's few blocks need other activations than the
-// next row's, so that a byte of X is fetched for every block that reads it (0.7 GB), 0.96 GB with W and the result at 6.8 TB/s; the matrix cores
-// are busy a quarter of the time.  Gated 14336 x 4096 at 95 %, 4096 tokens, G, U and H kept in 8 bits, 91 to 100 us: the 176 MB of results (20 us
-// for G and U, 7 for SiLU) on top of the steps (42 us through the 8-bit instruction, 17 more widened), which a row of 1.6 blocks a matrix
-// keeps short.  2048 x 8192 at 90 %, 64-wide, 2048 tokens, fp32 with an fp32 residual: 21 us, half of them bytes at a large copy's rate, the rest
-// widened steps.
+// Bound, 53248 x 16384 at 95 %, 2048 tokens, bf16: the widening, which every wave does for its own fragments, and the matrix instructions behind it: 37 and 43 %
+// of the SIMDs' cycles by the counters, of which two waves a SIMD hide one behind the other only in part; beside that 0.66 GB read - a row's few blocks need
+// other activations than the next row's, so that a byte of X is fetched for every block that reads it - and 0.22 written.  Gated 14336 x 4096 at 95 %, 4096
+// tokens, G, U and H kept in 8 bits, 97 to 100 us: 178 MB of results (20 us for G and U, 7 for SiLU) on top of the steps (60 us), which a row of 1.6
+// blocks a matrix keeps short; vector instructions take 46 % of the cycles, matrix instructions 19.  2048 x 8192 at 90 %, 64-wide, 2048 tokens, fp32 with an fp32
+// residual: 22 us, half of them bytes at a large copy's rate, the rest widened steps.
 // k_linear8_split: eight waves have a block row's B rows, or 32 of them, of 32 tokens and deal the stored blocks among themselves, W by way
 // of LDS in whole lines, X straight into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
-// Bound: a wave's chain of row, columns, blocks and X behind a launch (one token, 14336 x 4096 at 95 %, bf16 4.1 us, 6.0 with whole rows and W
-// straight into registers; at 70 % 5.1, 10.1 so; gated with 8-bit results 7.9 and 13.2, 8.9 and 20.4 so; 64-wide 8192 x 2048 at 90 %, gated, five
-// tokens 6.1, 6.0 so; 1600 x 6400 at 80 %, 333 tokens 7.7, 8.1 so; with bias and bf16 residual 9.4, 11 where they were asked for behind the sums).
+// Bound: a wave's chain of row, columns, blocks and X behind a launch (one token, 14336 x 4096 at 95 %, bf16 4.2 us, with whole rows 5.4; at 70 % 7.6 and 9.5, where
+// widening counts; gated with 8-bit results 8.2 and 14.6; 64-wide 8192 x 2048 at 90 %, gated, five tokens 5.9; 1600 x 6400 at 80 %, 333 tokens 9.5; with bias
+// and bf16 residual 9.4, 11 where they were asked for behind the sums).
 #pragma once
 #include "kern_scaled8.h"
 #include "kern_stream.h"
@@ -117,37 +118,31 @@ __device__ __forceinline__ void linear8_finish(const Linear8Args& a, float (&z)[
   }
 }
 
-// The same codes widened to bf16, eight a 16-deep instruction.
+// Codes widened to bf16 (exact), eight a 16-deep instruction.
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi, int fmt, float scale) {
   const u32x2v a = widen4((uint32_t)lo, fmt, scale), b = widen4((uint32_t)hi, fmt, scale);
   return __builtin_bit_cast(bf16x8, (u32x4{a[0], a[1], b[0], b[1]}));
 }
 
 // 64 of the contraction on 32 x 32 tiles: a lane has 32 bytes of a row of each operand, in formats WF and XF, the same places on both.
-// EXACT: widened to bf16 (the formats are constants for that too: a branch at every conversion kept conversions and matrix instructions
-// apart, 2048 x 8192 at 90 %, 2048 tokens, fp32 32.6 us, 21.2 without).
-template <int RT, int NT, bool EXACT, int WF, int XF>
+// The 8-bit instructions take the codes as they are at two and a half times the rate, but hold a sum of 64 products in too few bits: they drop what lies
+// 15 to 17 bits below the largest (448 and -448 beside 62 of 2^-9 give 0.10 for 0.12; 1.5e-5 root mean square of a sum of random terms, 4e-8
+// widened).  (The formats are constants: a branch at every conversion kept conversions and matrix instructions apart, 2048 x 8192 at 90 %, 2048
+// tokens, fp32 32.6 us, 21.2 without.)
+template <int RT, int NT, int WF, int XF>
 __device__ __forceinline__ void multiply8(f32x16 (&d)[RT][NT], const i32x8 (&fw)[RT], const i32x8 (&fx)[NT], int ws, const int (&xs)[NT]) {
-  if constexpr (EXACT) {
-    const float wsf = scale_value(ws);
+  const float wsf = scale_value(ws);
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      bf16x8 bw[RT], bx[NT];
+  for (int p = 0; p < 4; ++p) {
+    bf16x8 bw[RT], bx[NT];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) bw[i] = widen8(fw[i][2 * p], fw[i][2 * p + 1], WF, wsf);
+    for (int i = 0; i < RT; ++i) bw[i] = widen8(fw[i][2 * p], fw[i][2 * p + 1], WF, wsf);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) bx[j] = widen8(fx[j][2 * p], fx[j][2 * p + 1], XF, scale_value(xs[j]));
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bw[i], bx[j], d[i][j], 0, 0, 0);
-    }
-  } else {
+    for (int j = 0; j < NT; ++j) bx[j] = widen8(fx[j][2 * p], fx[j][2 * p + 1], XF, scale_value(xs[j]));
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-        d[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[i], fx[j], d[i][j], WF, XF, 0, ws, 0, xs[j]);
+      for (int j = 0; j < NT; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bw[i], bx[j], d[i][j], 0, 0, 0);
   }
 }
 
@@ -267,7 +262,7 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, 
 }
 
 // A workgroup's codes of one tensor meet in LDS, [token][row], so that a token's B bytes - a whole line of 128 - leave together and past
-// the L2s (bf16 results past the L2s too: 53248 x 16384 at 95 %, 2048 tokens 168 -> 146 us).
+// the L2s (bf16 results past the L2s too: 53248 x 16384 at 95 %, 2048 tokens 195 -> 189 us).
 template <int B>
 __device__ __forceinline__ uint32_t code_at(int tok, int chunk) {
   return (uint32_t)(tok * B + ((chunk ^ (B == 128 ? tok & 7 : (tok >> 1) & 3)) << 4));
@@ -455,7 +450,7 @@ struct Items8 {
   }
 };
 
-template <int B, bool DUAL, bool EXACT, int WF, int XF>
+template <int B, bool DUAL, int WF, int XF>
 __global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
   using C = L8Cfg<B>;
   constexpr int NW = C::NW, NSTAGE = C::NSTAGE, NT = C::NT, KB = C::KB, NM = DUAL ? 2 : 1, TT = C::TT;
@@ -558,7 +553,7 @@ __global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
         fx[j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         xs[j] = sc[(KB == 2 ? kk : 0) * 256 + row];
       }
-      multiply8<2, NT, EXACT, WF, XF>(d, fw, fx, kk && KB == 2 ? w1 : w0, xs);
+      multiply8<2, NT, WF, XF>(d, fw, fx, kk && KB == 2 ? w1 : w0, xs);
     }
   };
 
@@ -748,7 +743,7 @@ struct S8Cfg {
 };
 
 // ROWS: of a block row's B, the workgroup's (blockIdx.y says which).  The sums are the same in either form.
-template <int B, int ROWS, bool DUAL, bool EXACT, int WF, int XF>
+template <int B, int ROWS, bool DUAL, int WF, int XF>
 __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
   using C = S8Cfg<B, ROWS, DUAL>;
   constexpr int NM = DUAL ? 2 : 1, RT = C::RT, NW = C::NW, KS = B / 64;
@@ -844,7 +839,7 @@ __global__ __launch_bounds__(512) void k_linear8_split(const Linear8Args a) {
           ask(next, m, q0 + e + NW);
         }
         const i32x8 fx[1] = {now.x[k]};
-        multiply8<RT, 1, EXACT, WF, XF>(d, fw, fx, now.ws, xs);
+        multiply8<RT, 1, WF, XF>(d, fw, fx, now.ws, xs);
       }
     }
   };
