@@ -156,7 +156,8 @@ class Network:
         self.first -= rate * first
 
     def token_calls(self, h, x_out):
-        """The calls of one token (or a few) on kept buffers: h (fp32 [tokens, width]) is updated in place, x_out receives the output."""
+        """The calls of one token (or a few) on kept buffers: h (fp32 [tokens, width]) is updated in place, x_out receives the output.
+        Weights in 8 bits are made here, once: after a step the calls are prepared again."""
         t, calls = h.shape[0], []
         x = torch.empty((t, self.width), dtype=BF16, device="cuda")
         calls.append(api.prepare_norm_residual(h, None, h, x, weight=self.first))
@@ -168,6 +169,13 @@ class Network:
                 calls.append(api.prepare_bsr_linear(blk["w1"].packed, x, a, bias=blk["b1"], act="gelu"))
                 calls.append(api.prepare_bsr_linear(blk["w2"].packed, a, h, bias=blk["b2"], residual=h))
                 calls.append(api.prepare_norm_residual(h, None, h, out, **self._norm(blk)))
+            elif self.eight_bit:
+                x8, y = api.empty_scaled8(t, self.width, group=self.b), torch.empty((t, self.width), dtype=BF16, device="cuda")
+                inner = api.empty_scaled8(t, blk["gate"].packed.rows, group=self.b)
+                calls.append(api.prepare_quantize_scaled8(x, x8))
+                calls.append(api.prepare_bsr_gated_scaled8(blk["gate"].eight(), blk["up"].eight(), x8, inner))
+                calls.append(api.prepare_bsr_linear_scaled8(blk["down"].eight(), inner, y))
+                calls.append(api.prepare_norm_residual(h, y, h, out, **self._norm(blk)))
             else:
                 m = (blk["gate"].packed, blk["up"].packed, blk["down"].packed)
                 y = torch.empty((t, self.width), dtype=BF16, device="cuda")
@@ -195,18 +203,17 @@ def train(net, steps=30, tokens=512, rate=0.02, seed=1):
 
 
 def main():
-    losses = train(Network(eight_bit=True))
-    print("gated blocks in 8 bits: loss %.4f -> %.4f" % (losses[0], losses[-1]))
-    net = Network()
-    losses = train(net)
-    print("loss %.4f -> %.4f" % (losses[0], losses[-1]))
-    h = torch.randn((1, net.width), device="cuda")
-    want = net.forward(h.clone())
-    out = torch.empty((1, net.width), dtype=BF16, device="cuda")
-    for call in net.token_calls(h, out):
-        call()
-    torch.cuda.synchronize()
-    print("one token: off by %.3g of the forward pass" % float((out.float() - want.float()).abs().max()))
+    for eight_bit in (True, False):
+        net = Network(eight_bit=eight_bit)
+        losses = train(net)
+        print("%sloss %.4f -> %.4f" % ("gated blocks in 8 bits: " if eight_bit else "", losses[0], losses[-1]))
+        h = torch.randn((1, net.width), device="cuda")
+        want = net.forward(h.clone())
+        out = torch.empty((1, net.width), dtype=BF16, device="cuda")
+        for call in net.token_calls(h, out):
+            call()
+        torch.cuda.synchronize()
+        print("one token: off by %.3g of the forward pass" % float((out.float() - want.float()).abs().max()))
 
 
 if __name__ == "__main__":
