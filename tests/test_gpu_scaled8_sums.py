@@ -8,7 +8,7 @@ import torch
 
 from paper_2507_03117_amd import api
 from tests import scaled8_reference as ref
-from tests.test_gpu_scaled8 import BF16, F32, Matrix, activation, close, eight, gen, masks
+from tests.test_gpu_scaled8 import BF16, F32, Matrix, activation, close, close8, eight, gen, masks
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,18 @@ def test_no_term_of_a_long_row_is_lost(b, T):
     low = api.bsr_linear_scaled8(m.w8, q, out_dtype=BF16)
     assert torch.equal(low, y.to(BF16))
     assert rel(low, z) <= off + 2.0 ** -8 / 3 ** 0.5
+
+
+@pytest.mark.parametrize("b,T", [(64, 90), (64, 1), (128, 40)])
+def test_kept_intermediate_of_the_forward_pass(b, T):
+    """H, G and U of a gated block whose weights differ, against 64 bits."""
+    g = gen(5)
+    mg, mu = (Matrix(g, masks(4, 5, s), b, "e4m3") for s in (1, 2))
+    q, x = eight(activation(g, T, mg.cols, 0.3), b, "e4m3")
+    r = api.bsr_gated_scaled8(mg.w8, mu.w8, q, keep=True)
+    (zg, og, _), (zu, ou, _) = mg.product(x), mu.product(x)
+    close8(r.G, zg, og, "G")
+    close8(r.U, zu, ou, "U")
+    a = ref.act("silu", zg)
+    h = a * zu
+    close8(r.H, h, (1.13 * og + 2.0 ** -20 * zg.abs()) * (zu.abs() + ou) + a.abs() * ou + 2.0 ** -23 * h.abs(), "H")
