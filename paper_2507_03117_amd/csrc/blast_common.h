@@ -69,6 +69,9 @@ inline AuxLayout aux_layout(int64_t nbr, int64_t nbc, int64_t nnz) {
   return L;
 }
 
+// A launch counts its lanes in 32 bits and says nothing when there are more: workgroups of `threads` that one can have.
+constexpr int64_t most_groups(int threads) { return ((int64_t)1 << 31) / threads; }
+
 // One flag per device, set once something per-device has been done.  Host threads may race on it: the
 // worst outcome is that the (idempotent) action runs twice.
 struct DeviceFlags {

@@ -13,7 +13,7 @@ int check_keep(const void* X, int64_t ldx, int32_t dtype, int64_t T, int64_t K, 
   return BLAST_OK;
 }
 
-int keep_args(const void* X, int64_t ldx, int32_t dtype, int64_t T, int64_t K, const blast_scaled8_view* q, KeepArgs& a, bool& vec, int64_t& grid) {
+int keep_args(const void* X, int64_t ldx, int32_t dtype, int64_t T, int64_t K, const blast_scaled8_view* q, KeepArgs& a, bool& vec) {
   a.q = eight_of(q);
   a.x = X;
   a.ldx = ldx;
@@ -21,9 +21,22 @@ int keep_args(const void* X, int64_t ldx, int32_t dtype, int64_t T, int64_t K, c
   a.K = K;
   a.x_bf16 = dtype == BLAST_BF16;
   a.tiles = (int)((K + kKeepCols - 1) / kKeepCols);
-  grid = a.tiles * ((T + 4 * kKeepRows - 1) / (4 * kKeepRows));
   vec = K % 8 == 0 && blast::aligned(X, 16) && ldx * (a.x_bf16 ? 2 : 4) % 16 == 0 && blast::aligned(q->codes, 8) && q->ld % 8 == 0;
-  return grid > INT32_MAX ? BLAST_ERR_INVALID_ARG : BLAST_OK;
+  return a.tiles * ((T + 4 * kKeepRows - 1) / (4 * kKeepRows)) > INT32_MAX ? BLAST_ERR_INVALID_ARG : BLAST_OK;
+}
+
+// f(arguments, grid) for as many tokens at a time as a launch has lanes for.
+template <class F>
+void for_tokens(KeepArgs a, F&& f) {
+  constexpr int kRows = 4 * kKeepRows;
+  const int64_t all = a.T, most = blast::most_groups(256) / a.tiles * kRows;
+  for (int64_t t = 0; t < all; t += most) {
+    a.T = all - t < most ? all - t : most;
+    f(a, dim3((unsigned)(a.tiles * ((a.T + kRows - 1) / kRows))));
+    a.q.codes += most * a.q.ld;
+    a.q.scales += most;  // (a multiple of four: a wave's scales stay one word)
+    a.x = static_cast<const unsigned char*>(a.x) + most * a.ldx * (a.x_bf16 ? 2 : 4);
+  }
 }
 
 }  // namespace
@@ -33,22 +46,23 @@ extern "C" int blast_quantize_scaled8(const void* X, int64_t ldx, int32_t x_dtyp
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   if (int rc = check_keep(X, ldx, x_dtype, T, K, out)) return rc;
   if (T == 0 || K == 0) return BLAST_OK;
-  KeepArgs a{};
+  KeepArgs args{};
   bool vec = false;
-  int64_t grid = 0;
-  if (int rc = keep_args(X, ldx, x_dtype, T, K, out, a, vec, grid)) return rc;
-  const dim3 g((unsigned)grid), b(256);
-  if (out->group == 64) {
-    if (vec)
-      k_quantize_scaled8<64, true><<<g, b, 0, stream>>>(a);
-    else
-      k_quantize_scaled8<64, false><<<g, b, 0, stream>>>(a);
-  } else {
-    if (vec)
-      k_quantize_scaled8<128, true><<<g, b, 0, stream>>>(a);
-    else
-      k_quantize_scaled8<128, false><<<g, b, 0, stream>>>(a);
-  }
+  if (int rc = keep_args(X, ldx, x_dtype, T, K, out, args, vec)) return rc;
+  for_tokens(args, [&](const KeepArgs& a, dim3 g) {
+    const dim3 b(256);
+    if (out->group == 64) {
+      if (vec)
+        k_quantize_scaled8<64, true><<<g, b, 0, stream>>>(a);
+      else
+        k_quantize_scaled8<64, false><<<g, b, 0, stream>>>(a);
+    } else {
+      if (vec)
+        k_quantize_scaled8<128, true><<<g, b, 0, stream>>>(a);
+      else
+        k_quantize_scaled8<128, false><<<g, b, 0, stream>>>(a);
+    }
+  });
   BLAST_LAUNCH_CHECK("k_quantize_scaled8");
   return BLAST_OK;
 }
@@ -58,14 +72,15 @@ extern "C" int blast_dequantize_scaled8(const blast_scaled8_view* X, int64_t T, 
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   if (int rc = check_keep(Y, ldy, y_dtype, T, K, X)) return rc;
   if (T == 0 || K == 0) return BLAST_OK;
-  KeepArgs a{};
+  KeepArgs args{};
   bool vec = false;
-  int64_t grid = 0;
-  if (int rc = keep_args(Y, ldy, y_dtype, T, K, X, a, vec, grid)) return rc;
-  if (vec)
-    k_dequantize_scaled8<true><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(a);
-  else
-    k_dequantize_scaled8<false><<<dim3((unsigned)grid), dim3(256), 0, stream>>>(a);
+  if (int rc = keep_args(Y, ldy, y_dtype, T, K, X, args, vec)) return rc;
+  for_tokens(args, [&](const KeepArgs& a, dim3 g) {
+    if (vec)
+      k_dequantize_scaled8<true><<<g, dim3(256), 0, stream>>>(a);
+    else
+      k_dequantize_scaled8<false><<<g, dim3(256), 0, stream>>>(a);
+  });
   BLAST_LAUNCH_CHECK("k_dequantize_scaled8");
   return BLAST_OK;
 }
@@ -77,10 +92,15 @@ extern "C" int blast_bsr_quantize_scaled8(const blast_bsr_view* W, int32_t forma
   if (W->nnz == 0) return BLAST_OK;
   if (!W->vals || !blast::aligned(W->vals, 16) || !vals8 || !blast::aligned(vals8, 16) || !scales || !blast::aligned(scales, 16))
     return BLAST_ERR_INVALID_ARG;
-  if (W->b == 64)
-    k_quantize_blocks8<64><<<dim3((unsigned)W->nnz), dim3(256), 0, stream>>>(W->vals, W->nnz, format, vals8, scales);
-  else
-    k_quantize_blocks8<128><<<dim3((unsigned)W->nnz), dim3(256), 0, stream>>>(W->vals, W->nnz, format, vals8, scales);
+  const int64_t size = (int64_t)W->b * W->b, most = blast::most_groups(256);
+  for (int64_t q = 0; q < W->nnz; q += most) {
+    const int64_t n = W->nnz - q < most ? W->nnz - q : most;
+    const dim3 g((unsigned)n), b(256);
+    if (W->b == 64)
+      k_quantize_blocks8<64><<<g, b, 0, stream>>>(W->vals + q * size, n, format, vals8 + q * size, scales + q);
+    else
+      k_quantize_blocks8<128><<<g, b, 0, stream>>>(W->vals + q * size, n, format, vals8 + q * size, scales + q);
+  }
   BLAST_LAUNCH_CHECK("k_quantize_blocks8");
   return BLAST_OK;
 }
