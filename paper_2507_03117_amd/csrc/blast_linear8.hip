@@ -88,7 +88,9 @@ template <int B, bool DUAL, int WF, int XF>
 int launch_linear8(Linear8Args a, hipStream_t stream) {
   const int64_t tiles = (int64_t)a.nbr * (((int64_t)a.T + 127) / 128);
   static blast::DeviceFlags tile_set;
-  if (a.T <= 32 || tiles < kFewTiles<B, DUAL>) {
+  // (a workgroup of 512 lanes to a block row and 32 tokens: not more than a launch has lanes for; lists have any number)
+  const bool few = a.T <= 32 && a.nbr < blast::most_groups(512);
+  if (few || tiles < kFewTiles<B, DUAL>) {
     if (a.y8.codes || a.k8[0].codes || a.k8[1].codes) return launch_split<B, B, DUAL, WF, XF>(a, stream);
     const int64_t groups = (int64_t)a.nbr * (((int64_t)a.T + 31) / 32);
     if (a.T <= 32 || groups <= kFewGroups) return launch_split<B, 32, DUAL, WF, XF>(a, stream);
