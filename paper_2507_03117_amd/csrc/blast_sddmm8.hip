@@ -79,9 +79,12 @@ extern "C" int blast_bsr_sddmm_scaled8(const blast_bsr_view* W, const uint16_t* 
   if (!W->col_idx || !dvals || !blast::aligned(dvals, 16)) return BLAST_ERR_INVALID_ARG;
   const int b = W->b;
   const int64_t n = W->nnz * b * b;
-  const dim3 each((unsigned)((n / 4 + 255) / 256));
   if (T == 0) {  // an empty sum
-    k_zero_blocks<<<each, dim3(256), 0, stream>>>(dvals, n);
+    const int64_t most = blast::most_groups(256) * 1024;  // values of a launch
+    for (int64_t i = 0; i < n; i += most) {
+      const int64_t part = n - i < most ? n - i : most;
+      k_zero_blocks<<<dim3((unsigned)((part / 4 + 255) / 256)), dim3(256), 0, stream>>>(dvals + i, part);
+    }
     BLAST_LAUNCH_CHECK("k_zero_blocks");
     return BLAST_OK;
   }
@@ -102,14 +105,14 @@ extern "C" int blast_bsr_sddmm_scaled8(const blast_bsr_view* W, const uint16_t* 
   const bool split = runs > 1;
   if (split && (!ws || !blast::aligned(ws, 16) || ws_bytes < (size_t)runs * (size_t)n * 4)) return BLAST_ERR_WORKSPACE;
   const int64_t units = W->nnz * (b / 64) * (b / 64) * runs;
-  if (units > INT32_MAX - 64) return BLAST_ERR_INVALID_ARG;
+  if (units > blast::most_groups(64)) return BLAST_ERR_INVALID_ARG;  // (a wave at least to each: more lanes than a launch has)
   a.runs = (int)runs;
   a.n_units = (int)units;
   a.out = split ? static_cast<float*>(ws) : dvals;
   a.out_run = n;
   if (int rc = a.x.fmt == BLAST_E4M3 ? launch<BLAST_E4M3>(a, b, stream) : launch<BLAST_E5M2>(a, b, stream)) return rc;
   if (!split) return BLAST_OK;
-  k_join_runs<<<each, dim3(256), 0, stream>>>(a.out, n, a.runs, dvals, n);
+  k_join_runs<<<dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, stream>>>(a.out, n, a.runs, dvals, n);
   BLAST_LAUNCH_CHECK("k_join_runs");
   return BLAST_OK;
 }

@@ -1,4 +1,6 @@
 """Scaled 8-bit operands of more rows or blocks than one launch has lanes for (2^32)."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -62,3 +64,18 @@ def test_products_of_many_block_rows(out):
         codes[:, r] = 0
         q.scales[r, :T] = 27
     assert not codes.any() and bool((q.scales[:, :T] == 27).all())
+
+
+def test_gradient_of_many_blocks_over_no_tokens():
+    """2^22 blocks of 64 x 64 and one: 64 GiB of zeros, four values to a lane."""
+    b, nnz = 64, (1 << 22) + 1
+    row_ptr = torch.tensor([0, nnz], dtype=torch.int32, device="cuda")
+    col_idx = torch.arange(nnz, dtype=torch.int32, device="cuda")
+    out = torch.ones((nnz, b * b), device="cuda")
+    v = api.BsrView(b, nnz * b, b, 0, nnz, row_ptr.data_ptr(), col_idx.data_ptr(), None, None, None)
+    x = api.Scaled8View(None, nnz * b, None, 16, 0, 64)
+    rc = api.lib().blast_bsr_sddmm_scaled8(C.byref(v), None, b, C.byref(x), 0, out.data_ptr(), None, 0,
+                                           torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    for q in range(0, nnz, 1 << 19):
+        assert not out[q:q + (1 << 19)].any(), q
