@@ -97,9 +97,9 @@ extern "C" int blast_bsr_quantize_scaled8(const blast_bsr_view* W, int32_t forma
     const int64_t n = W->nnz - q < most ? W->nnz - q : most;
     const dim3 g((unsigned)n), b(256);
     if (W->b == 64)
-      k_quantize_blocks8<64><<<g, b, 0, stream>>>(W->vals + q * size, n, format, vals8 + q * size, scales + q);
+      k_quantize_blocks8<64><<<g, b, 0, stream>>>(W->vals + q * size, format, vals8 + q * size, scales + q);
     else
-      k_quantize_blocks8<128><<<g, b, 0, stream>>>(W->vals + q * size, n, format, vals8 + q * size, scales + q);
+      k_quantize_blocks8<128><<<g, b, 0, stream>>>(W->vals + q * size, format, vals8 + q * size, scales + q);
   }
   BLAST_LAUNCH_CHECK("k_quantize_blocks8");
   return BLAST_OK;

@@ -41,7 +41,7 @@ struct Linear8Args {
   Eight x;
   int wfmt;
   int T, nbr, ntt;
-  int parts;             // XCDs that share a block row, each with its own token tiles: 1, 2, 4 or 8
+  int parts;             // XCDs that share a block row, each with its own token tiles: 1 or 2
   int act;
   const float* bias;     // single matrix: all of these
   const void* r;
@@ -164,7 +164,7 @@ __device__ __forceinline__ int items8(const Linear8Args& a) {
 template <int B>
 struct L8Cfg {
   static_assert(B == 64 || B == 128, "");
-  static constexpr int NW = 4, NSTAGE = 2, TT = 32 * NW;  // tokens of a workgroup
+  static constexpr int NW = 4, TT = 32 * NW;  // tokens of a workgroup
   static constexpr int KB = 128 / B;            // stored blocks of a step
   static constexpr int WR = B / 64;             // waves along the rows, 64 each
   static constexpr int WT = NW / WR;            // waves along the tokens
@@ -172,10 +172,9 @@ struct L8Cfg {
   static constexpr int NT = TW / 32;
   static constexpr int W_BYTES = B * 128, X_BYTES = TT * 128;
   static constexpr int WI = W_BYTES / (1024 * NW), XI = X_BYTES / (1024 * NW);  // copy instructions of a wave, 1 KiB each
-  static constexpr int OPS = WI + XI + 1;       // with the one of the tokens' scales
   static constexpr int S_BYTES = KB * 256;
   static constexpr int STAGE = W_BYTES + X_BYTES + S_BYTES;
-  static constexpr int RING = NSTAGE * STAGE;
+  static constexpr int RING = 2 * STAGE;       // one step is multiplied, the next on its way
   static constexpr int EX_BYTES = 3 * WR * TT * 4;  // largest magnitudes that the waves of a token's rows tell each other
   static constexpr int LDS_BYTES = RING + EX_BYTES;
   static constexpr int OUT_BYTES = 4096;            // a wave's part of a stage when results leave
@@ -453,7 +452,7 @@ struct Items8 {
 template <int B, bool DUAL, int WF, int XF>
 __global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
   using C = L8Cfg<B>;
-  constexpr int NW = C::NW, NSTAGE = C::NSTAGE, NT = C::NT, KB = C::KB, NM = DUAL ? 2 : 1, TT = C::TT;
+  constexpr int NW = C::NW, NT = C::NT, KB = C::KB, NM = DUAL ? 2 : 1, TT = C::TT;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l32 = lane & 31, lh = lane >> 5;
@@ -470,9 +469,9 @@ __global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
 #pragma unroll
   for (int i = 0; i < C::WI; ++i) woff[i] = (uint32_t)(((i * NW + wave) * 8 + (lane >> 3)) * B) + coff;
 
-  // The loader runs NSTAGE - 1 steps ahead of the multiplier, over the same sequence of items, matrices and steps.
+  // The loader runs a step ahead of the multiplier, over the same sequence of items, matrices and steps.
   Items8<NM, TT> batch;
-  int l_item = -1, l_m = NM - 1, l_s = 0, l_kb = 0, l_nb = 0, l_t0 = 0, l_c0 = 0, l_c1 = 0, l_slot = 0, ahead = 0;
+  int l_item = -1, l_m = NM - 1, l_s = 0, l_kb = 0, l_nb = 0, l_t0 = 0, l_c0 = 0, l_c1 = 0, l_slot = 0;
   bool l_valid = true;
   const uint8_t* xrow[C::XI];
   int64_t soff = 0;
@@ -521,8 +520,7 @@ __global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
     __builtin_amdgcn_global_load_lds(
         (const __attribute__((address_space(1))) void*)(a.x.scales + (((int64_t)cs * B) >> a.x.shift) * a.x.lds + soff),
         (__attribute__((address_space(3))) void*)(st + C::W_BYTES + C::X_BYTES + which * 256), 4, 0, 0);
-    l_slot = l_slot + 1 == NSTAGE ? 0 : l_slot + 1;
-    ++ahead;
+    l_slot ^= 1;
     ++l_s;
     seek();
   };
@@ -571,27 +569,19 @@ __global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
       const bool two = KB == 2 && b0 + 1 < nb;
       const int w0 = (ld_idx(reinterpret_cast<const int*>(m.scales), q >> 2) >> (8 * (q & 3))) & 255;
       const int w1 = two ? (ld_idx(reinterpret_cast<const int*>(m.scales), (q + 1) >> 2) >> (8 * ((q + 1) & 3))) & 255 : w0;
-      // Copies retire in the order in which they were asked for: all but those of the steps after this one.  (__syncthreads would wait for
-      // those too.)
-      if (NSTAGE > 2 && ahead == NSTAGE - 1)
-        __builtin_amdgcn_s_waitcnt(BLAST_VMCNT((NSTAGE - 2) * C::OPS));
-      else
-        __builtin_amdgcn_s_waitcnt(BLAST_VMCNT(0));
+      __builtin_amdgcn_s_waitcnt(BLAST_VMCNT(0));  // this step's copies: no others are under way
       __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): what was read of the step before is here
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_barrier();  // everybody's copies of this step have landed, and the stage of the step before is free
       asm volatile("" ::: "memory");
-      --ahead;
       if (l_valid) issue();
       multiply(d, w0, w1, two, slot);
-      slot = slot + 1 == NSTAGE ? 0 : slot + 1;
+      slot ^= 1;
     }
   };
 
   seek();
-#pragma unroll 1
-  for (int g = 0; g < NSTAGE - 1; ++g)
-    if (l_valid) issue();
+  if (l_valid) issue();
 
   Items8<NM, TT> mine;
 #pragma unroll 1
@@ -614,7 +604,7 @@ __global__ __launch_bounds__(256, 2) void k_linear8(const Linear8Args a) {
     int ln = lane;
     asm volatile("" : "+v"(ln));  // (what follows from it is made here again, not kept in registers through the steps)
     const int l32 = ln & 31, lh = ln >> 5, thread = wave * 64 + ln;
-    unsigned char* stage = smem + (slot == 0 ? NSTAGE - 1 : slot - 1) * C::STAGE;
+    unsigned char* stage = smem + (slot ^ 1) * C::STAGE;
     unsigned char* lds = stage + wave * C::OUT_BYTES;
     uint32_t* ex = reinterpret_cast<uint32_t*>(smem + C::RING);
     const int64_t tw = t0 + wt * C::TW, row0 = (int64_t)r * B + wr * 64;

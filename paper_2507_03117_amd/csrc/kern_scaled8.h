@@ -235,7 +235,7 @@ __global__ __launch_bounds__(256) void k_dequantize_scaled8(const KeepArgs a) {
 // ---- the stored blocks of a weight, one scale each -----------------------------------------------------------------------------
 
 template <int B>
-__global__ __launch_bounds__(256) void k_quantize_blocks8(const uint16_t* vals, int64_t nnz, int fmt, uint8_t* codes, uint8_t* scales) {
+__global__ __launch_bounds__(256) void k_quantize_blocks8(const uint16_t* vals, int fmt, uint8_t* codes, uint8_t* scales) {
   constexpr int kPieces = B * B / 8 / 256;
   __shared__ uint32_t most[4];
   const int64_t q = blockIdx.x;
