@@ -12,8 +12,10 @@
 // of the SIMDs' cycles by the counters, of which two waves a SIMD hide one behind the other only in part; beside that 0.66 GB read - a row's few blocks need
 // other activations than the next row's, so that a byte of X is fetched for every block that reads it - and 0.22 written.  Gated 14336 x 4096 at 95 %, 4096
 // tokens, G, U and H kept in 8 bits, 97 to 100 us: 178 MB of results (20 us for G and U, 7 for SiLU) on top of the steps (60 us), which a row of 1.6
-// blocks a matrix keeps short; vector instructions take 46 % of the cycles, matrix instructions 19.  2048 x 8192 at 90 %, 64-wide, 2048 tokens, fp32 with an fp32
+// blocks a matrix keeps short; vector instructions take 44 % of the cycles, matrix instructions 19.  2048 x 8192 at 90 %, 64-wide, 2048 tokens, fp32 with an fp32
 // residual: 22 us, half of them bytes at a large copy's rate, the rest widened steps.
+// Registers: 128 (one 64-wide matrix) to 248 (a 128-wide pair), no vector spills in any instance; 25 to 49 scalars of the tile kernel, addresses that results
+// use, wait in lanes of a vector register.
 // k_linear8_split: eight waves have a block row's B rows, or 32 of them, of 32 tokens and deal the stored blocks among themselves, W by way
 // of LDS in whole lines, X straight into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
 // Bound: a wave's chain of row, columns, blocks and X behind a launch (one token, 14336 x 4096 at 95 %, bf16 4.2 us, with whole rows 5.4; at 70 % 7.6 and 9.5, where
