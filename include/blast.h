@@ -616,9 +616,10 @@ int blast_norm_residual_backward_workspace(const blast_norm_view* P, int64_t T, 
  * one in E5M2 and NaN in E4M3; a finite magnitude beyond 1.75 * 2^127 counts as that.  A group's scale is a byte from 27 to 246; other
  * bytes in what a call reads are not checked.
  *
- * What the form saves is memory: half of bf16's for weights and for what a step keeps.  Against the bf16 calls on the same shapes it saves time where bytes of W
- * or X are the bound (128-wide blocks at 2048 tokens: 0.72 to 0.93 of the bf16 product's time; one token through many blocks: 0.8) and takes longer where they
- * are not: 64-wide blocks at 2048 tokens 1.07 to 1.27, one token through few blocks 1.2, the gradient of the blocks 1.2.
+ * What the form saves is memory: half of bf16's for weights and for what a step keeps.  Against the bf16 calls on the same shapes it saves
+ * time where bytes of W or X are the bound (128-wide blocks at 2048 tokens: 0.72 to 0.93 of the bf16 product's time; one token through many
+ * blocks: 0.8) and takes longer where they are not: 64-wide blocks at 2048 tokens 1.07 to 1.27, one token through few blocks 1.2, the
+ * gradient of the blocks 1.2.
  */
 #define BLAST_E4M3 0 /* 4 exponent bits (bias 7), 3 of mantissa, no infinities, 0x7F / 0xFF NaN, largest value 448 */
 #define BLAST_E5M2 1 /* as in blast_quantize_e5m2, largest value 57344 */
@@ -664,9 +665,10 @@ int blast_bsr_quantize_scaled8(const blast_bsr_view* W, int32_t format, uint8_t*
  * The codes are widened exactly and multiplied by the 16-bit matrix instruction; sums are held in fp32, bias, activation and residual are
  * added in fp32, with one rounding when a value is stored: bf16 results are the fp32 ones rounded, 8-bit ones what blast_quantize_scaled8 makes of the
  * fp32 ones, and neither depends on what else the call writes.
- * Sums: no atomics; their order is fixed for the structure, b and T.  It is that of the blocks in a row where there are many tiles of 128 tokens, and that of
- * eight waves' partial sums where there are few, so that a token's last bits can change with the number of tokens beside it, and with it whether the product
- * is a call by itself or half of a gated pair.  Off by at most n 2^-24 of the sum of the n products' magnitudes.
+ * Sums: no atomics; their order is fixed for the structure, b and T.  It is that of the blocks in a row where there are many tiles of 128
+ * tokens, and that of eight waves' partial sums where there are few, so that a token's last bits can change with the number of tokens
+ * beside it, and with it whether the product is a call by itself or half of a gated pair.  Off by at most n 2^-24 of the sum of the n
+ * products' magnitudes.
  * No output overlaps another or an input, R = Y apart.
  * Never synchronises.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED_BLOCK, HIP.
  */
@@ -678,8 +680,8 @@ int blast_bsr_linear_scaled8(const blast_bsr_view* W, const blast_weight8_view* 
  * The gated half of Eq. (1) in one launch:  G = Wgate X,  U = Wup X,  H = act(G) (.) U.
  *   H, ldh              out, bf16 [T][rows]
  *   H8                  out, scaled 8-bit, group = b; exactly one of H and H8 is given
- *   G8, U8              out, likewise, each may be NULL: what the gradients of the blocks and blast_act_backward_scaled8 read.  The activation takes G and U before they are
- *                       rounded.
+ *   G8, U8              out, likewise, each may be NULL: what the gradients of the blocks and blast_act_backward_scaled8 read.  The
+ *                       activation takes G and U before they are rounded.
  * act, operands, arithmetic and errors as in blast_bsr_linear_scaled8;
  * BLAST_ACT_NONE is a product of the two.  Wgate and Wup have one shape, block width and format.
  */

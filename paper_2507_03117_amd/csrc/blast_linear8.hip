@@ -7,19 +7,20 @@ using namespace blast_dev;
 
 namespace {
 
-// Fewer 128-token tiles than this are cut into tiles of 32 whose blocks eight waves share, and up to 32 tokens any number.  Microseconds
-// of 128-token tiles / of 32, bf16 results (8-bit ones within 4 %, fp32 ones 1 to 5 us more on both sides), with the number of the former.  64-wide,
-// 2048 x 8192 at 90 %, 64 tiles 13.8 / 6.7, 192: 14.7 / 12.8, 256: 15.1 / 14.6, 288: 16.0 / 16.9; 6400 x 1600 at 80 %, 200: 9.0 / 7.8, 300: 9.3 / 10.6; 1600 x
-// 6400 at 80 %, 225: 18.7 / 18.0, 250: 18.9 / 19.4; 8192 x 2048 at 50 %, 256, a tile to a CU: 16.2 / 14.7.  Gated, 2048 x 8192, 128: 22.8 / 17.2, 192: 23.6 / 23.9;
-// 6400 x 1600, 100: 13.3 / 10.7, 200: 14.0 / 19.4.  128-wide, 4096 x 14336 at 95 %, 128: 16.7 / 12.9, 192: 16.8 / 17.9, at 70 %, 128: 49 / 31, 192: 49 / 45, 224:
-// 50 / 55; 14336 x 4096 at 95 %, 112: 9.8 / 7.8, 224: 10.7 / 13.9; gated 112: 16.7 / 16.7, at 70 % 38 / 32; 4096 x 14336, 128: 27.4 / 27.6, at 70 % 91 / 62.
+// Fewer 128-token tiles than this are cut into tiles of 32 whose blocks eight waves share, and up to 32 tokens any number.  Microseconds of
+// 128-token tiles / of 32, bf16 results (8-bit ones within 4 %, fp32 ones 1 to 5 us more on both sides), with the number of the former.
+// 64-wide, 2048 x 8192 at 90 %, 64 tiles 13.8 / 6.7, 192: 14.7 / 12.8, 256: 15.1 / 14.6, 288: 16.0 / 16.9; 6400 x 1600 at 80 %, 200: 9.0 /
+// 7.8, 300: 9.3 / 10.6; 1600 x 6400 at 80 %, 225: 18.7 / 18.0, 250: 18.9 / 19.4; 8192 x 2048 at 50 %, 256, a tile to a CU: 16.2 / 14.7.
+// Gated, 2048 x 8192, 128: 22.8 / 17.2, 192: 23.6 / 23.9; 6400 x 1600, 100: 13.3 / 10.7, 200: 14.0 / 19.4.  128-wide, 4096 x 14336 at 95 %,
+// 128: 16.7 / 12.9, 192: 16.8 / 17.9, at 70 %, 128: 49 / 31, 192: 49 / 45, 224: 50 / 55; 14336 x 4096 at 95 %, 112: 9.8 / 7.8, 224: 10.7 /
+// 13.9; gated 112: 16.7 / 16.7, at 70 % 38 / 32; 4096 x 14336, 128: 27.4 / 27.6, at 70 % 91 / 62.
 template <int B, bool DUAL>
 constexpr int64_t kFewTiles = B == 64 && !DUAL ? 256 : 144;
 
-// Workgroups that have 32 rows of a block row each, where no scale needs all of them: up to 32 tokens, and where whole rows would be this many
-// workgroups or fewer (us, 32 rows / whole; bf16; one token: 14336 x 4096 at 95 % 4.2 / 5.4, at 70 % 7.6 / 9.5, 4096 x 14336 at 95 % 4.2 / 6.5, 64-wide
-// 8192 x 2048 at 90 % 3.7 / 4.1; 100 tokens: 4096 x 14336 at 95 %, 128 whole ones 6.9 / 7.2, at 70 % 17.9 / 16.8, 64-wide 2048 x 8192 at 90 % 5.2 / 5.6; 14336 x 4096 at
-// 95 %, 448: 9.4 / 7.7, 64-wide 8192 x 2048, 512: 6.2 / 5.0).
+// Workgroups that have 32 rows of a block row each, where no scale needs all of them: up to 32 tokens, and where whole rows would be this
+// many workgroups or fewer (us, 32 rows / whole; bf16; one token: 14336 x 4096 at 95 % 4.2 / 5.4, at 70 % 7.6 / 9.5, 4096 x 14336 at 95 %
+// 4.2 / 6.5, 64-wide 8192 x 2048 at 90 % 3.7 / 4.1; 100 tokens: 4096 x 14336 at 95 %, 128 whole ones 6.9 / 7.2, at 70 % 17.9 / 16.8,
+// 64-wide 2048 x 8192 at 90 % 5.2 / 5.6; 14336 x 4096 at 95 %, 448: 9.4 / 7.7, 64-wide 8192 x 2048, 512: 6.2 / 5.0).
 constexpr int64_t kFewGroups = 128;
 
 int check_weight(const blast_bsr_view* W, const blast_weight8_view* W8) {
@@ -50,8 +51,9 @@ int cu_count8() {
 }
 
 // Workgroups for tiles of TT tokens: one for each, or as many as are resident at once; 0: more tiles than can be counted.  Many tiles: two
-// XCDs share a block row, each with half of its tokens (us, one / two / four / eight XCDs to a row: 53248 x 16384 at 95 %, 2048 tokens 191 / 189 / 191 /
-// 192; gated 14336 x 4096, 4096 tokens 99 / 100 / 100 / 99; 2048 x 8192 at 90 %, 64-wide, 2048 tokens 24.0 / 22.8 / 22.2 / 22.0).  An odd number of tiles leaves one of two XCDs a tile short.
+// XCDs share a block row, each with half of its tokens (us, one / two / four / eight XCDs to a row: 53248 x 16384 at 95 %, 2048 tokens 191
+// / 189 / 191 / 192; gated 14336 x 4096, 4096 tokens 99 / 100 / 100 / 99; 2048 x 8192 at 90 %, 64-wide, 2048 tokens 24.0 / 22.8 / 22.2 /
+// 22.0).  An odd number of tiles leaves one of two XCDs a tile short.
 int64_t grid8(Linear8Args& a, int TT, int64_t resident) {
   a.ntt = (int)(((int64_t)a.T + TT - 1) / TT);
   a.parts = TT >= 128 && a.ntt >= 2 && (a.ntt % 2 == 0 || a.ntt >= 16) ? 2 : 1;

@@ -4,23 +4,24 @@
 //
 // k_linear8: workgroups of four waves, two on a CU, walk lists of tiles: a block row's B rows of 128 tokens.  A step is 128 of the
 // contraction: a stored block of 128 x 128 or two of 64 x 64, W and X tiles copied to LDS in rows of 128 bytes, the scales of the step's
-// tokens beside them; the next step's copies are under way while one is multiplied, the next tile's first step while a tile's results
-// leave (passes on the GPU alone: 53248 x 16384 at 95 %, 2048 tokens, a workgroup for each tile 199 us, lists 189; gated 14336 x 4096, 4096 tokens, 106 /
-// 100).
+// tokens beside them; the next step's copies are under way while one is multiplied, the next tile's first step while a tile's results leave
+// (passes on the GPU alone: 53248 x 16384 at 95 %, 2048 tokens, a workgroup for each tile 199 us, lists 189; gated 14336 x 4096, 4096
+// tokens, 106 / 100).
 //
-// Bound, 53248 x 16384 at 95 %, 2048 tokens, bf16: the widening, which every wave does for its own fragments, and the matrix instructions behind it: 37 and 43 %
-// of the SIMDs' cycles by the counters, of which two waves a SIMD hide one behind the other only in part; beside that 0.66 GB read - a row's few blocks need
-// other activations than the next row's, so that a byte of X is fetched for every block that reads it - and 0.22 written.  Gated 14336 x 4096 at 95 %, 4096
-// tokens, G, U and H kept in 8 bits, 97 to 100 us: 178 MB of results (20 us for G and U, 7 for SiLU) on top of the steps (60 us), which a row of 1.6
-// blocks a matrix keeps short; vector instructions take 44 % of the cycles, matrix instructions 19.  2048 x 8192 at 90 %, 64-wide, 2048 tokens, fp32 with an fp32
-// residual: 22 us, half of them bytes at a large copy's rate, the rest widened steps.
-// Registers: 128 (one 64-wide matrix) to 248 (a 128-wide pair), no vector spills in any instance; 25 to 49 scalars of the tile kernel, addresses that results
-// use, wait in lanes of a vector register.
+// Bound, 53248 x 16384 at 95 %, 2048 tokens, bf16: the widening, which every wave does for its own fragments, and the matrix instructions
+// behind it: 37 and 43 % of the SIMDs' cycles by the counters, of which two waves a SIMD hide one behind the other only in part; beside
+// that 0.66 GB read - a row's few blocks need other activations than the next row's, so that a byte of X is fetched for every block that
+// reads it - and 0.22 written.  Gated 14336 x 4096 at 95 %, 4096 tokens, G, U and H kept in 8 bits, 97 to 100 us: 178 MB of results (20 us
+// for G and U, 7 for SiLU) on top of the steps (60 us), which a row of 1.6 blocks a matrix keeps short; vector instructions take 44 % of
+// the cycles, matrix instructions 19.  2048 x 8192 at 90 %, 64-wide, 2048 tokens, fp32 with an fp32 residual: 22 us, half of them bytes at
+// a large copy's rate, the rest widened steps.
+// Registers: 128 (one 64-wide matrix) to 248 (a 128-wide pair), no vector spills in any instance; 25 to 49 scalars of the tile kernel,
+// addresses that results use, wait in lanes of a vector register.
 // k_linear8_split: eight waves have a block row's B rows, or 32 of them, of 32 tokens and deal the stored blocks among themselves, W by way
 // of LDS in whole lines, X straight into registers; their sums meet in LDS.  For calls whose 128-token tiles would leave CUs without work.
-// Bound: a wave's chain of row, columns, blocks and X behind a launch (one token, 14336 x 4096 at 95 %, bf16 4.2 us, with whole rows 5.4; at 70 % 7.6 and 9.5, where
-// widening counts; gated with 8-bit results 8.2 and 14.6; 64-wide 8192 x 2048 at 90 %, gated, five tokens 5.9; 1600 x 6400 at 80 %, 333 tokens 9.5; with bias
-// and bf16 residual 9.4, 11 where they were asked for behind the sums).
+// Bound: a wave's chain of row, columns, blocks and X behind a launch (one token, 14336 x 4096 at 95 %, bf16 4.2 us, with whole rows 5.4;
+// at 70 % 7.6 and 9.5, where widening counts; gated with 8-bit results 7.9 and 13.1; 64-wide 8192 x 2048 at 90 %, gated, five tokens 6.2;
+// 1600 x 6400 at 80 %, 333 tokens 9.5; with bias and bf16 residual 9.7, 11 where they were asked for behind the sums).
 #pragma once
 #include "kern_scaled8.h"
 #include "kern_stream.h"
@@ -126,11 +127,11 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi, int fmt, float scale) {
   return __builtin_bit_cast(bf16x8, (u32x4{a[0], a[1], b[0], b[1]}));
 }
 
-// 64 of the contraction on 32 x 32 tiles: a lane has 32 bytes of a row of each operand, in formats WF and XF, the same places on both.
-// The 8-bit instructions take the codes as they are at two and a half times the rate, but hold a sum of 64 products in too few bits: they drop what lies
-// 15 to 17 bits below the largest (448 and -448 beside 62 of 2^-9 give 0.10 for 0.12; 1.5e-5 root mean square of a sum of random terms, 4e-8
-// widened).  (The formats are constants: a branch at every conversion kept conversions and matrix instructions apart, 2048 x 8192 at 90 %, 2048
-// tokens, fp32 32.6 us, 21.2 without.)
+// 64 of the contraction on 32 x 32 tiles: a lane has 32 bytes of a row of each operand, in formats WF and XF, the same places on both.  The
+// 8-bit instructions take the codes as they are at two and a half times the rate, but hold a sum of 64 products in too few bits: they drop
+// what lies 15 to 17 bits below the largest (448 and -448 beside 62 of 2^-9 give 0.10 for 0.12; 1.5e-5 root mean square of a sum of random
+// terms, 4e-8 widened).  (The formats are constants: a branch at every conversion kept conversions and matrix instructions apart, 2048 x
+// 8192 at 90 %, 2048 tokens, fp32 32.6 us, 21.2 without.)
 template <int RT, int NT, int WF, int XF>
 __device__ __forceinline__ void multiply8(f32x16 (&d)[RT][NT], const i32x8 (&fw)[RT], const i32x8 (&fx)[NT], int ws, const int (&xs)[NT]) {
   const float wsf = scale_value(ws);

@@ -5,9 +5,9 @@
 // activations is read once a block.  A stage is 32 tokens: dY as it is and X widened on the way into LDS, both turned by the
 // transposing LDS read.  Two stages are on their way in registers, the next is converted beside this one's matrix instructions.
 // Bound: a stage's chain of LDS write, barrier, LDS read and matrix instructions, 0.5 us alone on a CU and 0.8 for two workgroups there, of
-// which the matrix cores have 0.13 (179 blocks, 4096 tokens: 49 us with the joining of two runs, 6 of them, and 58 with inputs from
-// memory; 75 before anything ran ahead, 66 with one stage ahead, 60 with conflicting LDS rows).  Its 358 workgroups of two runs leave 154 of 256 CUs with one
-// and 102 with two: stages dealt evenly would be 90 to a CU instead of up to 128.
+// which the matrix cores have 0.13 (179 blocks, 4096 tokens: 49 us with the joining of two runs, 6 of them, and 58 with inputs from memory;
+// 75 before anything ran ahead, 66 with one stage ahead, 60 with conflicting LDS rows).  Its 358 workgroups of two runs leave 154 of 256
+// CUs with one and 102 with two: stages dealt evenly would be 90 to a CU instead of up to 128.
 //
 // k_sddmm8_units (64-wide blocks; 128-wide ones where few have a middling number of tokens): a unit is a 64 x 64 part of a block and a
 // run of tokens.  KW waves share it (four: they deal its stages of 16 tokens, and their sums meet in LDS in wave order; one: it has them
